@@ -73,7 +73,9 @@ typedef enum {
     GDN_ERR_WORKSPACE = -3,     /* workspace missing or smaller than gdn_workspace_size() */
     GDN_ERR_CUDA = -4,          /* a CUDA runtime / driver call failed */
     GDN_ERR_TIMEOUT = -5,       /* device-side bounded wait expired (status_word only) */
-    GDN_ERR_TOO_LARGE = -6      /* more requests than the built-in scratch of the no-allocation entry holds */
+    GDN_ERR_TOO_LARGE = -6,     /* more requests than the built-in scratch of the no-allocation entry holds */
+    GDN_ERR_BAD_INDEX = -7,     /* a slot, page or row named by device data does not exist or may not be used so (status_word only) */
+    GDN_ERR_NO_PAGES = -8       /* gdn_cache_fork found too few free pages (status_word only) */
 } gdn_status;
 
 typedef enum { GDN_F32 = 0, GDN_BF16 = 1 } gdn_dtype;
@@ -210,6 +212,150 @@ GDN_API int32_t gdn_tail_replay_static_scratch(const gdn_desc* desc, const void*
  */
 GDN_API int64_t tail_select(int64_t prefix_len, double budget_frac);
 
+/*
+ * ---- Recurrent layers beside the Gated DeltaNet: short convolution and selective scan ----
+ *
+ * What stands before and beside the recurrence above in hybrid models.  Device pointers only.  Prompts are packed as above
+ * (cu_tail_lens: request n owns rows [cu[n], cu[n+1])); total_tokens may exceed cu[num_seqs] (a padded batch): rows from
+ * cu[num_seqs] on are neither read nor written.  Row strides are in elements, between consecutive tokens; the last dimension is
+ * packed.  Any alignment is served; the vector path needs 16-byte aligned rows.  The states lie in pools:
+ *     convolution  [slots, width - 1, channels] in io_dtype: the last width - 1 input rows, oldest first
+ *     scan         [slots, channels, states] fp32
+ * Request n starts from slot init_slots[n] of init_state and leaves its state in slot out_slots[n] of out_state (NULL: slot n).  A
+ * negative init slot is a zero start, a negative out slot keeps no state.  init_state == NULL starts all from zero, out_state ==
+ * NULL keeps none.  The two pools may be the same memory: a request may write the slot that it reads, but no slot that another
+ * request of the call reads or writes.  A slot outside the pool counts as a negative one and sets GDN_ERR_BAD_INDEX in
+ * *status_word (if given).  A request without tokens hands its start state on.
+ */
+typedef struct gdn_conv_desc {
+    int32_t  channels;          /* C >= 1 */
+    int32_t  width;             /* K: 2, 3 or 4 */
+    int32_t  io_dtype;          /* gdn_dtype of x, weight, bias, out and the states */
+    int32_t  num_seqs;          /* N */
+    int64_t  total_tokens;      /* rows of x and out (gdn_short_conv) */
+    int64_t  x_stride, out_stride;
+    int32_t  silu;              /* 1: SiLU on the result, 0: none */
+    int32_t  num_init_states, num_out_states;  /* slots in the two pools */
+    int32_t  reserved;          /* 0 */
+    const int32_t* init_slots;  /* [N] device int32, or NULL */
+    const int32_t* out_slots;   /* [N] device int32, or NULL */
+    int32_t* status_word;       /* optional device int32; written only on an error in device data */
+    void*    stream;            /* cudaStream_t */
+} gdn_conv_desc;
+
+/*
+ * Depthwise causal convolution over each request's rows and the width - 1 rows before them (its start state):
+ *     out[t,c] = act(bias[c] + sum_j weight[c,j] x[t - width + 1 + j, c])         weight [C, width], bias [C] or NULL
+ * accumulated in fp32, rounded once.  out may not overlap x.
+ */
+GDN_API int32_t gdn_short_conv(const gdn_conv_desc* desc, const void* x, const void* weight, const void* bias,
+                               const int32_t* cu_tail_lens, const void* init_state, void* out, void* out_state);
+
+/*
+ * The same for one token per request: x and out [N, C].  Request n has slot init_slots[n] (NULL: n) of both pools; one with a
+ * negative slot is padding, whose row of out and states are left as they were.  out_slots and total_tokens are ignored.  out may be
+ * x, state_out may be state_in.
+ */
+GDN_API int32_t gdn_short_conv_step(const gdn_conv_desc* desc, const void* x, const void* weight, const void* bias,
+                                    const void* state_in, void* out, void* state_out);
+
+typedef struct gdn_scan_desc {
+    int32_t  channels;          /* C >= 1 */
+    int32_t  states;            /* S: 8, 16, 32 or 64 */
+    int32_t  groups;            /* G, a divisor of C: channel i reads b and c of group i / (C / G) */
+    int32_t  io_dtype;          /* gdn_dtype of x, dt, b, c, z and out */
+    int32_t  num_seqs;          /* N */
+    int32_t  softplus;          /* 1: dt = softplus(dt + dt_bias), 0: dt + dt_bias */
+    int64_t  total_tokens;
+    int64_t  x_stride, dt_stride, b_stride, c_stride, z_stride, out_stride;
+    int32_t  num_init_states, num_out_states;
+    const int32_t* init_slots;
+    const int32_t* out_slots;
+    int32_t* status_word;
+    void*    stream;
+} gdn_scan_desc;
+
+/*
+ * Selective state space scan, per request and channel i with state h in R^S (fp32 throughout, outputs rounded once):
+ *     dt'  = softplus(dt[t,i] + dt_bias[i])
+ *     h[s] = exp(dt' a[i,s]) h[s] + dt' x[t,i] b[t,g,s]
+ *     out[t,i] = (sum_s c[t,g,s] h[s] + d[i] x[t,i]) * silu(z[t,i])
+ * x, dt, z, out [T, C]; b, c [T, G, S]; a [C, S], d, dt_bias [C] fp32, packed.  d, z and dt_bias may be NULL (no skip, no gate, no
+ * bias).  out may be x, dt or z itself (the same address and stride), and overlap none of them otherwise.
+ */
+GDN_API int32_t gdn_selective_scan(const gdn_scan_desc* desc, const void* x, const void* dt, const float* a, const void* b, const void* c,
+                                   const float* d, const void* z, const float* dt_bias, const int32_t* cu_tail_lens,
+                                   const float* init_state, void* out, float* out_state);
+
+/* The same for one token per request: x, dt, z, out [N, C], b, c [N, G, S]; slots as in gdn_short_conv_step. */
+GDN_API int32_t gdn_selective_scan_step(const gdn_scan_desc* desc, const void* x, const void* dt, const float* a, const void* b,
+                                        const void* c, const float* d, const void* z, const float* dt_bias, const float* state_in,
+                                        void* out, float* state_out);
+
+/*
+ * ---- Pages of a cache ----
+ *
+ * A prefix hit begins as a branch of the matched request: its attention layers' key/value pages are shared, its recurrent states
+ * copied.  A cache is a set of pools (one per layer, say), each of num_pages pages; page p of the cache is page p of every pool.
+ * refcounts [num_pages] int32 says how many table rows hold a page (0: free); tables [num_rows, row_pages] int32 holds each
+ * request's pages in order, -1 where there is none.  All of it is device memory of the caller's; the calls allocate nothing, read
+ * nothing back and can be captured.  The bookkeeping depends on nothing but its inputs: free pages are taken from the lowest number up.
+ * Calls on one cache must follow one another (one stream, or streams ordered by events).
+ */
+typedef struct gdn_pool {
+    void*   base;               /* num_pages pages of page_bytes, packed; 16-byte aligned */
+    int64_t page_bytes;         /* a multiple of 16 */
+} gdn_pool;
+
+typedef struct gdn_cache_desc {
+    const gdn_pool* pools;      /* host array of num_pools entries, read during the call */
+    int32_t  num_pools;
+    int32_t  num_pages;
+    int32_t  page_tokens;       /* tokens in a page (gdn_cache_fork) */
+    int32_t  num_rows, row_pages;
+    int32_t  reserved;          /* 0 */
+    void*    workspace;         /* device scratch of gdn_cache_fork and gdn_cache_compact, 256-byte aligned */
+    size_t   workspace_bytes;   /* >= gdn_cache_workspace_size() */
+    int32_t* status_word;       /* optional device int32; written only on an error in device data */
+    void*    stream;
+} gdn_cache_desc;
+
+/* Device scratch of a call with `count` forks (gdn_cache_compact: 0).  One call at a time may use it, as gdn_workspace_size says. */
+GDN_API size_t gdn_cache_workspace_size(const gdn_cache_desc* desc, int32_t count);
+
+/*
+ * Page src[i] to page dst[i], in every pool, for i < count.  The dst pages must differ from each other and from all src pages.  A
+ * pair that names no page is left out (GDN_ERR_BAD_INDEX).  src, dst: device int32.
+ */
+GDN_API int32_t gdn_cache_copy(const gdn_cache_desc* desc, const int32_t* src, const int32_t* dst, int32_t count);
+
+/*
+ * Row children[i] becomes a branch of row parents[i] after tokens[i] tokens, for i < count: the pages that the child held are given
+ * back; the tokens / page_tokens whole pages are shared (their counts go up); where tokens end inside a page, that page is copied to a
+ * free one, which the child alone holds; the rest of the child's row is -1.  All children give back before any takes a page.
+ * A child may be named once and may not be a parent in the same call; tokens fit the row; the parent holds pages for them.  A fork that
+ * breaks this is left out, its child's row as it was (GDN_ERR_BAD_INDEX).  Too few free pages: the forks that get none, the last ones
+ * that need one, leave their child's row empty (GDN_ERR_NO_PAGES).  At most GDN_CACHE_MAX_ROWS rows.
+ */
+#define GDN_CACHE_MAX_ROWS 262144
+GDN_API int32_t gdn_cache_fork(const gdn_cache_desc* desc, int32_t* refcounts, int32_t* tables, const int32_t* parents,
+                               const int32_t* children, const int32_t* tokens, int32_t count);
+
+/*
+ * The rows rows[i], i < count, give their pages back: counts go down, the entries become -1.  A row named twice is given back once.  An
+ * entry that names no page, or a free one, becomes -1 and sets GDN_ERR_BAD_INDEX.  The pools are not touched (num_pools may be 0).
+ */
+GDN_API int32_t gdn_cache_free(const gdn_cache_desc* desc, int32_t* refcounts, int32_t* tables, const int32_t* rows, int32_t count);
+
+/*
+ * The live pages (count above 0) brought to the front: with M of them, the k-th live page at or after M moves into the k-th free
+ * page below M.  out_refcounts and out_tables receive the counts and tables afterwards (they may be the inputs; where they are not,
+ * the old tables stay valid to read by until the pages moved from are written again), page_map [num_pages] each page's new number
+ * (-1: free), live [1] M.  A table entry that names no live page becomes -1 (GDN_ERR_BAD_INDEX).
+ */
+GDN_API int32_t gdn_cache_compact(const gdn_cache_desc* desc, const int32_t* refcounts, const int32_t* tables, int32_t* out_refcounts,
+                                  int32_t* out_tables, int32_t* page_map, int32_t* live);
+
 /* Static, human-readable text for a gdn_status value. */
 GDN_API const char* gdn_status_string(int32_t status);
 
@@ -224,7 +370,7 @@ GDN_API const char* gdn_status_string(int32_t status);
  */
 GDN_API void gdn_test_hooks(uint64_t wait_timeout_ns, int32_t skip_kq_load_of_chunk);
 
-/* Number of kernels the last forward call on this thread enqueued (for launch accounting). */
+/* Number of kernels the last call on this thread enqueued (for launch accounting). */
 GDN_API int32_t gdn_last_launch_count(void);
 
 #ifdef __cplusplus

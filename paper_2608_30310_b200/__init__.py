@@ -11,9 +11,15 @@ from ._binding import (  # noqa: F401
     gdn_tail_replay, gdn_full_prefill, gdn_tail_replay_static_scratch, gdn_decode_step, last_launch_count, Workspace,
     test_hooks,
 )
+from ._layers import (  # noqa: F401
+    gdn_short_conv, gdn_short_conv_step, gdn_selective_scan, gdn_selective_scan_step,
+    gdn_cache_copy, gdn_cache_fork, gdn_cache_free, gdn_cache_compact,
+)
 
 __all__ = [
     "GdnDesc", "GdnError", "library_path", "load_library", "status_string", "tail_select",
     "workspace_size", "gdn_tail_replay", "gdn_full_prefill", "gdn_tail_replay_static_scratch", "gdn_decode_step",
     "last_launch_count", "Workspace",
+    "gdn_short_conv", "gdn_short_conv_step", "gdn_selective_scan", "gdn_selective_scan_step",
+    "gdn_cache_copy", "gdn_cache_fork", "gdn_cache_free", "gdn_cache_compact",
 ]

@@ -71,6 +71,8 @@ def load_library():
     lib.gdn_last_launch_count.argtypes = []
     lib.gdn_test_hooks.restype = None
     lib.gdn_test_hooks.argtypes = [ctypes.c_uint64, ctypes.c_int32]
+    from . import _layers
+    _layers.declare(lib)
     _bind_native(lib)
     _lib = lib
     return lib
@@ -95,6 +97,8 @@ def _bind_native(lib):
     ext.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in
                ("gdn_tail_replay", "gdn_full_prefill", "gdn_tail_replay_static_scratch", "gdn_decode_step", "gdn_workspace_size")),
              Workspace)
+    from . import _layers
+    ext.bind_layers(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _layers.ENTRIES))
     _native = ext
 
 

@@ -377,6 +377,8 @@ const char* gdn_status_string(int32_t status)
         case GDN_ERR_CUDA: return "CUDA call failed";
         case GDN_ERR_TIMEOUT: return "device-side wait timed out";
         case GDN_ERR_TOO_LARGE: return "more requests than the built-in scratch holds";
+        case GDN_ERR_BAD_INDEX: return "an index in device data names nothing usable";
+        case GDN_ERR_NO_PAGES: return "too few free pages";
         default: return "unknown status";
     }
 }
@@ -384,3 +386,5 @@ const char* gdn_status_string(int32_t status)
 int32_t gdn_last_launch_count(void) { return g_last_launches; }
 
 }  // extern "C"
+
+namespace gdn { void set_launch_count(int n) { g_last_launches = n; } }

@@ -98,6 +98,8 @@ __device__ __forceinline__ int4 request_at(const Problem& p, const Sched& s, con
     return make_int4(p.cu[n], p.cu[n + 1], n, 0);
 }
 
+void set_launch_count(int n);             // what gdn_last_launch_count() answers on this thread
+
 cudaError_t launch_scheduler(const int32_t* cu, int32_t num_seqs, const Sched& s, cudaStream_t stream);
 cudaError_t launch_simt(const Problem& p, const Sched& s, int io_dtype, cudaStream_t stream, int* launches);
 // Whether the tensor-core path can run this problem; launch_tcgen05 returns cudaErrorNotSupported when it cannot.

@@ -1,0 +1,57 @@
+// What the kernels of the recurrent layers (short convolution, selective scan) and of the cache's pages share.
+#pragma once
+#include "common.cuh"
+
+namespace gdn {
+
+// The io dtype's values as fp32, and back with one rounding (to nearest even).
+template <typename T> __device__ __forceinline__ float widen(T x);
+template <> __device__ __forceinline__ float widen<float>(float x) { return x; }
+template <> __device__ __forceinline__ float widen<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T round_to(float x);
+template <> __device__ __forceinline__ float round_to<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 round_to<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// N consecutive values, moved 16 bytes at a time (less where there are fewer).
+template <typename T, int N> struct alignas(sizeof(T) * N % 16 == 0 ? 16 : sizeof(T) * N % 8 == 0 ? 8 : sizeof(T) * N % 4 == 0 ? 4 : 2) Pack {
+    T v[N];
+};
+
+// x sigmoid(x); the quotient's error is two steps of fp32, below what any output keeps
+__device__ __forceinline__ float silu_of(float x) { return __fdividef(x, 1.f + __expf(-x)); }
+
+// slots[n] (no list: n) where the pool has it, else -1; a slot past the pool's end is reported
+__device__ __forceinline__ int slot_of(const int32_t* slots, int n, int num_slots, int32_t* status_word)
+{
+    const int s = slots ? slots[n] : n;
+    if (s < num_slots) return s < 0 ? -1 : s;
+    if (status_word) *status_word = GDN_ERR_BAD_INDEX;
+    return -1;
+}
+
+// Arguments of the short convolution; all device pointers.
+struct ConvArgs {
+    const void *x, *weight, *bias, *init_state;
+    void *out, *out_state;
+    const int32_t *cu, *init_slots, *out_slots;
+    int32_t* status_word;
+    int64_t x_stride, out_stride, total_tokens;
+    int32_t channels, num_seqs, num_init, num_out, silu;
+};
+cudaError_t launch_conv(const ConvArgs& a, int io_dtype, int width, bool step, cudaStream_t stream);
+
+// Arguments of the selective scan; all device pointers.
+struct ScanArgs {
+    const void *x, *dt, *b, *c, *z;
+    const float *a, *d, *dt_bias, *init_state;
+    void* out;
+    float* out_state;
+    const int32_t *cu, *init_slots, *out_slots;
+    int32_t* status_word;
+    int64_t x_stride, dt_stride, b_stride, c_stride, z_stride, out_stride, total_tokens;
+    int32_t channels, groups, num_seqs, num_init, num_out, softplus;
+};
+cudaError_t launch_scan(const ScanArgs& a, int io_dtype, int states, cudaStream_t stream);
+cudaError_t launch_scan_step(const ScanArgs& a, int io_dtype, int states, cudaStream_t stream);
+
+}  // namespace gdn

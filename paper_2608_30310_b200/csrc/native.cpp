@@ -7,6 +7,8 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <c10/cuda/CUDAStream.h>
+#include <string.h>
+#include <initializer_list>
 #include "gdn_tail_replay.h"
 
 namespace {
@@ -180,7 +182,290 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// ---- recurrent layers and cache pages: all device tensors, on the current device
+
+struct Library {
+    int32_t (*conv)(const gdn_conv_desc*, const void*, const void*, const void*, const int32_t*, const void*, void*, void*);
+    int32_t (*conv_step)(const gdn_conv_desc*, const void*, const void*, const void*, const void*, void*, void*);
+    int32_t (*scan)(const gdn_scan_desc*, const void*, const void*, const float*, const void*, const void*, const float*, const void*, const float*,
+                    const int32_t*, const float*, void*, float*);
+    int32_t (*scan_step)(const gdn_scan_desc*, const void*, const void*, const float*, const void*, const void*, const float*, const void*, const float*,
+                         const float*, void*, float*);
+    int32_t (*copy)(const gdn_cache_desc*, const int32_t*, const int32_t*, int32_t);
+    int32_t (*fork)(const gdn_cache_desc*, int32_t*, int32_t*, const int32_t*, const int32_t*, const int32_t*, int32_t);
+    int32_t (*free)(const gdn_cache_desc*, int32_t*, int32_t*, const int32_t*, int32_t);
+    int32_t (*compact)(const gdn_cache_desc*, const int32_t*, const int32_t*, int32_t*, int32_t*, int32_t*, int32_t*);
+    size_t (*workspace_size)(const gdn_cache_desc*, int32_t);
+};
+Library g_lib = {};
+
+constexpr int64_t kMost = 0x7fffffff;
+
+// A tensor of this call: on the device, of the type and shape.  `any` sizes are taken as they are.
+constexpr int64_t kAny = -1;
+struct Args {
+    c10::DeviceIndex device = c10::cuda::current_device();
+    bool ok = true;
+
+    const at::Tensor* take(PyObject* o, at::ScalarType dt, bool optional, std::initializer_list<int64_t> shape)
+    {
+        if (optional && o == Py_None) return nullptr;
+        const at::Tensor* t = tensor(o);
+        ok = ok && t && t->is_cuda() && t->device().index() == device && t->scalar_type() == dt && t->dim() == (int64_t)shape.size();
+        for (size_t i = 0; ok && i < shape.size(); ++i) {
+            const int64_t want = shape.begin()[i], got = t->size((int64_t)i);
+            ok = got <= kMost && (want == kAny || want == got);
+        }
+        return ok ? t : nullptr;
+    }
+    const at::Tensor* packed(PyObject* o, at::ScalarType dt, std::initializer_list<int64_t> shape, bool optional = false)
+    {
+        const at::Tensor* t = take(o, dt, optional, shape);
+        ok = ok && (!t || t->is_contiguous());
+        return ok ? t : nullptr;
+    }
+    // rows of packed values, `stride` apart
+    const at::Tensor* rows(PyObject* o, at::ScalarType dt, std::initializer_list<int64_t> shape, int64_t& stride, bool optional = false)
+    {
+        const at::Tensor* t = take(o, dt, optional, shape);
+        stride = 0;
+        if (!ok || !t) return nullptr;
+        int64_t values = 1;
+        for (int64_t i = t->dim() - 1; i > 0; --i) {
+            ok = ok && (t->size(i) == 1 || t->stride(i) == values);
+            values *= t->size(i);
+        }
+        stride = t->size(0) > 1 ? t->stride(0) : values;
+        ok = ok && stride >= values;
+        return ok ? t : nullptr;
+    }
+    int32_t* status(PyObject* o)
+    {
+        if (o == Py_None) return nullptr;
+        const at::Tensor* t = tensor(o);
+        ok = ok && t && t->is_cuda() && t->device().index() == device && t->nbytes() >= 4;
+        return ok ? (int32_t*)t->data_ptr() : nullptr;
+    }
+    // the Workspace's buffer for the stream, if it is large enough (held by `b` over the call)
+    bool workspace(PyObject* o, void* stream, size_t need, Ref& b, void*& base, size_t& bytes)
+    {
+        if ((PyObject*)Py_TYPE(o) != g_workspace_type) return false;
+        const Ref map{PyObject_GetAttr(o, s_by_stream)}, key{PyLong_FromVoidPtr(stream)};
+        if (map.o && key.o && PyDict_Check(map.o)) b.o = PyDict_GetItemWithError(map.o, key.o);
+        Py_XINCREF(b.o);
+        PyErr_Clear();
+        const at::Tensor* buf = b.o ? tensor(b.o) : nullptr;
+        if (!buf || !buf->is_cuda() || buf->device().index() != device || buf->element_size() != 1) return false;
+        const uintptr_t at = (uintptr_t)buf->data_ptr(), off = (256 - at % 256) % 256;
+        if ((size_t)buf->numel() < need + off) return false;
+        base = (void*)(at + off);
+        bytes = (size_t)buf->numel() - off;
+        return true;
+    }
+};
+
+bool io_type(const at::Tensor* x, at::ScalarType& dt, int32_t& io)
+{
+    if (!x) return false;
+    dt = x->scalar_type();
+    io = dt == at::kBFloat16 ? GDN_BF16 : GDN_F32;
+    return dt == at::kBFloat16 || dt == at::kFloat;
+}
+
+// conv(step, x, weight, bias, cu_tail_lens, init_state, out, out_state, silu, init_slots, out_slots, status_word, stream)
+PyObject* conv(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 13 || !g_lib.conv) Py_RETURN_NONE;
+    const bool step = a[0] == Py_True;
+    const at::Tensor *x = tensor(a[1]), *w = tensor(a[2]);
+    at::ScalarType dt;
+    gdn_conv_desc d = {};
+    if (!io_type(x, dt, d.io_dtype) || !w || x->dim() != 2 || w->dim() != 2 || (a[8] != Py_True && a[8] != Py_False)) Py_RETURN_NONE;
+    const int64_t T = x->size(0), C = x->size(1), K = w->size(1);
+    Args g;
+    g.rows(a[1], dt, {kAny, kAny}, d.x_stride);
+    g.packed(a[2], dt, {C, kAny});
+    const at::Tensor* bias = g.packed(a[3], dt, {C}, true);
+    const at::Tensor* cu = step ? nullptr : g.packed(a[4], at::kInt, {kAny});
+    const at::Tensor* in = g.packed(a[5], dt, {kAny, K - 1, C}, !step);
+    const at::Tensor* out = g.rows(a[6], dt, {T, C}, d.out_stride);
+    const at::Tensor* keep = g.packed(a[7], dt, {kAny, K - 1, C}, !step);
+    if (!g.ok || C < 1 || K < 2 || (cu && cu->size(0) < 1)) Py_RETURN_NONE;
+    const int64_t N = step ? T : cu->size(0) - 1;
+    const at::Tensor *is = g.packed(a[9], at::kInt, {N}, true), *os = g.packed(a[10], at::kInt, {N}, true);
+    d.status_word = g.status(a[11]);
+    if (!g.ok || !stream_of(a[12], d.stream)) Py_RETURN_NONE;
+    d.channels = (int32_t)C; d.width = (int32_t)K; d.num_seqs = (int32_t)N; d.total_tokens = T; d.silu = a[8] == Py_True;
+    d.num_init_states = in ? (int32_t)in->size(0) : 0; d.num_out_states = keep ? (int32_t)keep->size(0) : 0;
+    d.init_slots = (const int32_t*)ptr(is); d.out_slots = (const int32_t*)ptr(os);
+    const void *px = ptr(x), *pw = ptr(w), *pb = ptr(bias), *pi = ptr(in);
+    const int32_t* pc = (const int32_t*)ptr(cu);
+    void *po = ptr(out), *pk = ptr(keep);
+    return without_gil([&]() { return step ? g_lib.conv_step(&d, px, pw, pb, pi, po, pk) : g_lib.conv(&d, px, pw, pb, pc, pi, po, pk); });
+}
+
+// scan(step, x, dt, a, b, c, d, z, dt_bias, cu_tail_lens, init_state, out, out_state, softplus, init_slots, out_slots, status_word, stream)
+PyObject* scan(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 18 || !g_lib.scan) Py_RETURN_NONE;
+    const bool step = a[0] == Py_True;
+    const at::Tensor *x = tensor(a[1]), *ta = tensor(a[3]), *b = tensor(a[4]);
+    at::ScalarType dt;
+    gdn_scan_desc d = {};
+    if (!io_type(x, dt, d.io_dtype) || !ta || !b || x->dim() != 2 || ta->dim() != 2 || b->dim() != 3 || (a[13] != Py_True && a[13] != Py_False))
+        Py_RETURN_NONE;
+    const int64_t T = x->size(0), C = x->size(1), S = ta->size(1), G = b->size(1);
+    Args g;
+    g.rows(a[1], dt, {kAny, kAny}, d.x_stride);
+    const at::Tensor* tdt = g.rows(a[2], dt, {T, C}, d.dt_stride);
+    g.packed(a[3], at::kFloat, {C, kAny});
+    g.rows(a[4], dt, {T, kAny, S}, d.b_stride);
+    const at::Tensor* c = g.rows(a[5], dt, {T, G, S}, d.c_stride);
+    const at::Tensor *skip = g.packed(a[6], at::kFloat, {C}, true), *z = g.rows(a[7], dt, {T, C}, d.z_stride, true), *bias = g.packed(a[8], at::kFloat, {C}, true);
+    const at::Tensor* cu = step ? nullptr : g.packed(a[9], at::kInt, {kAny});
+    const at::Tensor* in = g.packed(a[10], at::kFloat, {kAny, C, S}, !step);
+    const at::Tensor* out = g.rows(a[11], dt, {T, C}, d.out_stride);
+    const at::Tensor* keep = g.packed(a[12], at::kFloat, {kAny, C, S}, !step);
+    if (!g.ok || C < 1 || (cu && cu->size(0) < 1)) Py_RETURN_NONE;
+    const int64_t N = step ? T : cu->size(0) - 1;
+    const at::Tensor *is = g.packed(a[14], at::kInt, {N}, true), *os = g.packed(a[15], at::kInt, {N}, true);
+    d.status_word = g.status(a[16]);
+    if (!g.ok || !stream_of(a[17], d.stream)) Py_RETURN_NONE;
+    d.channels = (int32_t)C; d.states = (int32_t)S; d.groups = (int32_t)G; d.num_seqs = (int32_t)N; d.total_tokens = T; d.softplus = a[13] == Py_True;
+    d.num_init_states = in ? (int32_t)in->size(0) : 0; d.num_out_states = keep ? (int32_t)keep->size(0) : 0;
+    d.init_slots = (const int32_t*)ptr(is); d.out_slots = (const int32_t*)ptr(os);
+    const void *px = ptr(x), *pd = ptr(tdt), *pb = ptr(b), *pc = ptr(c), *pz = ptr(z);
+    const float *pa = (const float*)ptr(ta), *ps = (const float*)ptr(skip), *pt = (const float*)ptr(bias), *pi = (const float*)ptr(in);
+    const int32_t* pcu = (const int32_t*)ptr(cu);
+    void* po = ptr(out);
+    float* pk = (float*)ptr(keep);
+    return without_gil([&]() {
+        return step ? g_lib.scan_step(&d, px, pd, pa, pb, pc, ps, pz, pt, pi, po, pk) : g_lib.scan(&d, px, pd, pa, pb, pc, ps, pz, pt, pcu, pi, po, pk);
+    });
+}
+
+constexpr Py_ssize_t kPools = 256;           // more go through the general path
+// A list or tuple of pools [pages, ...], packed and with the same number of pages.
+bool pools_of(PyObject* o, Args& g, gdn_pool* pools, gdn_cache_desc& d)
+{
+    const bool list = PyList_Check(o);
+    if (!list && !PyTuple_Check(o)) return false;
+    const Py_ssize_t n = list ? PyList_GET_SIZE(o) : PyTuple_GET_SIZE(o);
+    if (n < 1 || n > kPools) return false;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        const at::Tensor* t = tensor(list ? PyList_GET_ITEM(o, i) : PyTuple_GET_ITEM(o, i));
+        if (!t || !t->is_cuda() || t->device().index() != g.device || t->dim() < 2 || !t->is_contiguous() || t->size(0) < 1 || t->size(0) > kMost) return false;
+        if (i == 0) d.num_pages = (int32_t)t->size(0);
+        if (t->size(0) != d.num_pages) return false;
+        pools[i].base = t->data_ptr();
+        pools[i].page_bytes = (int64_t)(t->nbytes() / (size_t)t->size(0));
+    }
+    d.pools = pools;
+    d.num_pools = (int32_t)n;
+    return true;
+}
+
+// cache_copy(pools, src, dst, status_word, stream)
+PyObject* cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 5 || !g_lib.copy) Py_RETURN_NONE;
+    Args g;
+    gdn_pool pools[kPools];
+    gdn_cache_desc d = {};
+    if (!pools_of(a[0], g, pools, d)) Py_RETURN_NONE;
+    const at::Tensor* src = g.packed(a[1], at::kInt, {kAny});
+    if (!g.ok) Py_RETURN_NONE;
+    const at::Tensor* dst = g.packed(a[2], at::kInt, {src->size(0)});
+    d.status_word = g.status(a[3]);
+    if (!g.ok || !stream_of(a[4], d.stream)) Py_RETURN_NONE;
+    const int32_t *ps = (const int32_t*)ptr(src), *pd = (const int32_t*)ptr(dst), count = (int32_t)src->size(0);
+    return without_gil([&]() { return g_lib.copy(&d, ps, pd, count); });
+}
+
+// cache_fork(pools, page_tokens, refcounts, tables, parents, children, tokens, workspace, status_word, stream)
+PyObject* cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 10 || !g_lib.fork) Py_RETURN_NONE;
+    Args g;
+    gdn_pool pools[kPools];
+    gdn_cache_desc d = {};
+    const long tokens = PyLong_AsLong(a[1]);
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    if (tokens < 1 || tokens > kMost || !pools_of(a[0], g, pools, d)) Py_RETURN_NONE;
+    const at::Tensor* counts = g.packed(a[2], at::kInt, {(int64_t)d.num_pages});
+    const at::Tensor* tables = g.packed(a[3], at::kInt, {kAny, kAny});
+    const at::Tensor* parents = g.packed(a[4], at::kInt, {kAny});
+    if (!g.ok) Py_RETURN_NONE;
+    const int64_t count = parents->size(0);
+    const at::Tensor *children = g.packed(a[5], at::kInt, {count}), *upto = g.packed(a[6], at::kInt, {count});
+    d.status_word = g.status(a[8]);
+    if (!g.ok || !stream_of(a[9], d.stream)) Py_RETURN_NONE;
+    d.page_tokens = (int32_t)tokens; d.num_rows = (int32_t)tables->size(0); d.row_pages = (int32_t)tables->size(1);
+    Ref held{nullptr};
+    if (!g.workspace(a[7], d.stream, g_lib.workspace_size(&d, (int32_t)count), held, d.workspace, d.workspace_bytes)) Py_RETURN_NONE;
+    int32_t *pc = (int32_t*)ptr(counts), *pt = (int32_t*)ptr(tables);
+    const int32_t *pp = (const int32_t*)ptr(parents), *pk = (const int32_t*)ptr(children), *pn = (const int32_t*)ptr(upto);
+    return without_gil([&]() { return g_lib.fork(&d, pc, pt, pp, pk, pn, (int32_t)count); });
+}
+
+// cache_free(refcounts, tables, rows, status_word, stream)
+PyObject* cache_free(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 5 || !g_lib.free) Py_RETURN_NONE;
+    Args g;
+    gdn_cache_desc d = {};
+    const at::Tensor *counts = g.packed(a[0], at::kInt, {kAny}), *tables = g.packed(a[1], at::kInt, {kAny, kAny}), *rows = g.packed(a[2], at::kInt, {kAny});
+    d.status_word = g.status(a[3]);
+    if (!g.ok || !stream_of(a[4], d.stream)) Py_RETURN_NONE;
+    d.num_pages = (int32_t)counts->size(0); d.num_rows = (int32_t)tables->size(0); d.row_pages = (int32_t)tables->size(1);
+    int32_t *pc = (int32_t*)ptr(counts), *pt = (int32_t*)ptr(tables);
+    const int32_t *pr = (const int32_t*)ptr(rows), count = (int32_t)rows->size(0);
+    return without_gil([&]() { return g_lib.free(&d, pc, pt, pr, count); });
+}
+
+// cache_compact(pools, refcounts, tables, out_refcounts, out_tables, page_map, live, workspace, status_word, stream)
+PyObject* cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 10 || !g_lib.compact) Py_RETURN_NONE;
+    Args g;
+    gdn_pool pools[kPools];
+    gdn_cache_desc d = {};
+    if (!pools_of(a[0], g, pools, d)) Py_RETURN_NONE;
+    const int64_t P = d.num_pages;
+    const at::Tensor *counts = g.packed(a[1], at::kInt, {P}), *tables = g.packed(a[2], at::kInt, {kAny, kAny});
+    if (!g.ok) Py_RETURN_NONE;
+    const at::Tensor *oc = g.packed(a[3], at::kInt, {P}), *ot = g.packed(a[4], at::kInt, {tables->size(0), tables->size(1)}),
+                     *map = g.packed(a[5], at::kInt, {P}), *live = g.packed(a[6], at::kInt, {1});
+    d.status_word = g.status(a[8]);
+    if (!g.ok || !stream_of(a[9], d.stream)) Py_RETURN_NONE;
+    d.num_rows = (int32_t)tables->size(0); d.row_pages = (int32_t)tables->size(1);
+    Ref held{nullptr};
+    if (!g.workspace(a[7], d.stream, g_lib.workspace_size(&d, 0), held, d.workspace, d.workspace_bytes)) Py_RETURN_NONE;
+    const int32_t *pc = (const int32_t*)ptr(counts), *pt = (const int32_t*)ptr(tables);
+    int32_t *qc = (int32_t*)ptr(oc), *qt = (int32_t*)ptr(ot), *qm = (int32_t*)ptr(map), *ql = (int32_t*)ptr(live);
+    return without_gil([&]() { return g_lib.compact(&d, pc, pt, qc, qt, qm, ql); });
+}
+
+// bind_layers(the addresses of the functions, in the order of Library's)
+PyObject* bind_layers(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    void* p[9];
+    if (n != 9) { PyErr_SetString(PyExc_TypeError, "nine addresses"); return nullptr; }
+    for (int i = 0; i < 9; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    static_assert(sizeof p == sizeof g_lib, "one address each");
+    memcpy(&g_lib, p, sizeof p);
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
+    {"conv", (PyCFunction)(void (*)(void))guarded<conv>, METH_FASTCALL, nullptr},
+    {"scan", (PyCFunction)(void (*)(void))guarded<scan>, METH_FASTCALL, nullptr},
+    {"cache_copy", (PyCFunction)(void (*)(void))guarded<cache_copy>, METH_FASTCALL, nullptr},
+    {"cache_fork", (PyCFunction)(void (*)(void))guarded<cache_fork>, METH_FASTCALL, nullptr},
+    {"cache_free", (PyCFunction)(void (*)(void))guarded<cache_free>, METH_FASTCALL, nullptr},
+    {"cache_compact", (PyCFunction)(void (*)(void))guarded<cache_compact>, METH_FASTCALL, nullptr},
+    {"bind_layers", (PyCFunction)(void (*)(void))bind_layers, METH_FASTCALL, nullptr},
     {"forward", (PyCFunction)(void (*)(void))guarded<forward>, METH_FASTCALL, nullptr},
     {"decode", (PyCFunction)(void (*)(void))guarded<decode>, METH_FASTCALL, nullptr},
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
