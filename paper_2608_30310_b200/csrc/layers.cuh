@@ -17,8 +17,22 @@ template <typename T, int N> struct alignas(sizeof(T) * N % 16 == 0 ? 16 : sizeo
     T v[N];
 };
 
-// x sigmoid(x); the quotient's error is two steps of fp32, below what any output keeps
-__device__ __forceinline__ float silu_of(float x) { return __fdividef(x, 1.f + __expf(-x)); }
+// 2^x and 1 / x by the special-function unit, each within two steps of fp32
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+// x sigmoid(x)
+__device__ __forceinline__ float silu_of(float x) { return x * rcp(1.f + ex2(-kLog2e * x)); }
 
 // slots[n] (no list: n) where the pool has it, else -1; a slot past the pool's end is reported
 __device__ __forceinline__ int slot_of(const int32_t* slots, int n, int num_slots, int32_t* status_word)

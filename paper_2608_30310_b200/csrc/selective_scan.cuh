@@ -1,42 +1,18 @@
-// Selective state space scan over packed prompts, one warp per tile of channels of a request:
+// Selective state space scan over packed prompts, one CTA per tile of channels of a request:
 //
 //     h = exp(dt a) h + dt x b,   y = c . h + d x,   out = y silu(z),   dt = softplus(dt + dt_bias)
 //
-// The state stays in registers from a request's first token to its last.  A lane holds SS states of CC channels (EPL = SS CC), LN =
-// S / SS lanes share CC channels, a warp has W = 32 CC / LN of them.  It goes through the request in blocks of TB rows:
-//   1. lane = (row, VE channels): softplus(dt + dt_bias) and dt x, once for every (row, channel), into shared memory;
-//   2. lane = (channels, states): the recurrence, row by row.  c . h is summed over the LN lanes TS rows at a time by exchanging
-//      halves, after which every lane holds some finished sums, so that n sums over LN lanes cost less than n exchanges;
-//   3. lane = (row, VE channels) again: skip, gate, rounding, store.
-// x, dt, z of the next block are loaded into registers, b and c copied to shared memory, under the current one.  Warps share nothing.
+// The state stays in registers from a request's first token to its last.  Four compute warps do the recurrence alone: a lane holds SS
+// states of CC channels, LN = S / SS lanes share CC channels.  c . h is summed over the LN lanes TS rows at a time by exchanging
+// halves, after which every lane holds some finished sums, so that n sums over LN lanes cost less than n exchanges.  Four helper
+// warps run around them, in blocks of TB rows: they copy x, dt, z, b and c of the block after the next but one to shared memory, form dt
+// and dt x of the next block (once for every row and channel), and finish the block before: skip, gate, rounding, store.  One
+// barrier per block.
 #pragma once
 #include "layers.cuh"
 
 namespace gdn {
 namespace scan {
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// log(1 + e^x).  log1p(u) = 2 atanh(u / (2 + u)): the odd series in s = u / (2 + u) <= 1/3, cut where the next term is below half a
-// step of fp32; a logarithm of 1 + u itself would lose the small time steps that e^x << 1 stands for.
-__device__ __forceinline__ float softplus_of(float x)
-{
-    const float u = __expf(-fabsf(x)), s = __fdividef(u, 2.f + u), q = s * s;
-    float p = fmaf(q, 2.f / 15.f, 2.f / 13.f);
-    p = fmaf(q, p, 2.f / 11.f);
-    p = fmaf(q, p, 2.f / 9.f);
-    p = fmaf(q, p, 2.f / 7.f);
-    p = fmaf(q, p, 2.f / 5.f);
-    p = fmaf(q, p, 2.f / 3.f);
-    p = fmaf(q, p, 2.f);
-    return fmaf(s, p, fmaxf(x, 0.f));
-}
 
 // ---- pairs of fp32 values in one register pair (add, multiply, fma on both at once)
 struct F2 { unsigned long long v; };
@@ -64,13 +40,48 @@ __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
     return r;
 }
-
-// asynchronous copies to shared memory; a size of 0 fills with zeros
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-template <int B> __device__ __forceinline__ void copy_async(void* dst, const void* src, bool there)
+__device__ __forceinline__ F2 add(F2 a, F2 b)
 {
-    if (B == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(there ? 4 : 0) : "memory");
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 both(float a) { return pair(a, a); }
+
+// log(1 + e^x) = max(x, 0) + log1p(u), u = e^-|x| in (0, 1].  log1p(u) / u is the polynomial of degree eight nearest to it (least largest
+// relative error, 3e-8, by Lawson's iteration); a logarithm of 1 + u would lose the small time steps that u << 1 stands for.
+__device__ __forceinline__ F2 softplus_of(F2 x2)
+{
+    const float2 x = parts(x2);
+    const F2 u = pair(ex2(-kLog2e * fabsf(x.x)), ex2(-kLog2e * fabsf(x.y)));
+    F2 p = fma(u, both(0.005232692641f), both(-0.02950523219f));
+    p = fma(u, p, both(0.07822594086f));
+    p = fma(u, p, both(-0.136632448f));
+    p = fma(u, p, both(0.191060062f));
+    p = fma(u, p, both(-0.2484298196f));
+    p = fma(u, p, both(0.3331909665f));
+    p = fma(u, p, both(-0.4999949302f));
+    p = fma(u, p, both(0.9999999694f));
+    return fma(u, p, pair(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
+}
+__device__ __forceinline__ float softplus_of(float x) { return parts(softplus_of(both(x))).x; }
+using ::gdn::silu_of;
+__device__ __forceinline__ F2 silu_of(F2 x)
+{
+    const float2 e = parts(mul(x, both(-kLog2e))), s = parts(add(pair(ex2(e.x), ex2(e.y)), both(1.f)));
+    return mul(x, pair(rcp(s.x), rcp(s.y)));
+}
+
+// values v and v + 1 of a pack
+template <typename T, int N> __device__ __forceinline__ F2 pair_at(const Pack<T, N>& p, int v) { return pair(widen<T>(p.v[v]), widen<T>(p.v[v + 1])); }
+
+// asynchronous copies to shared memory
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+template <int B> __device__ __forceinline__ void copy_async(void* dst, const void* src)
+{
+    static_assert(B == 4 || B == 8 || B == 16, "");
+    if (B == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_addr(dst)), "l"(src), "n"(B) : "memory");
 }
 
 template <typename T, int N> __device__ __forceinline__ void load_values(const T* p, float (&v)[N])
@@ -80,58 +91,220 @@ template <typename T, int N> __device__ __forceinline__ void load_values(const T
     for (int i = 0; i < N; ++i) v[i] = widen<T>(q.v[i]);
 }
 
+constexpr int kCompute = 4, kHelpers = 4, kThreads = 32 * (kCompute + kHelpers), kRing = 4;
+
 template <int S_, int SS_, int CC_, typename T> struct Form {
     static constexpr int S = S_, SS = SS_, CC = CC_;
-    static constexpr int LN = S / SS, W = 32 * CC / LN;
-    static constexpr int VE = W < 8 ? W : 8;                 // channels of an item
-    static constexpr int TB = 32 * VE / W;                   // rows of a block: one item per lane
-    static constexpr int TS = LN / CC > 4 ? LN / CC : (TB < 4 ? TB : 4);
+    static constexpr int LN = S / SS, W = 32 * CC / LN, CT = kCompute * W;      // channels of a warp, of the CTA
+    static constexpr int TS = LN / CC > 4 ? LN / CC : 4;     // rows of a reduction
+    static constexpr int TB = 32;                             // rows of a block
     static constexpr int SUMS = TS * CC, MINE = SUMS / LN;   // sums of a reduction, and how many a lane ends up with
-    static_assert(TB % TS == 0 && SUMS % LN == 0 && W * LN == 32 * CC, "");
-    static constexpr int PS = 2 * W + 4, YS = W + 4;         // row strides: the lanes of an item-wise access hit different banks
+    static constexpr int PER = TB * CT / (32 * kHelpers);    // channels of a row that a helper has in hand at once
+    static constexpr int VE = PER > 8 ? 8 : PER < 2 ? 2 : PER, ROWI = CT / VE, ITEMS = TB * ROWI, IPT = (ITEMS + 32 * kHelpers - 1) / (32 * kHelpers);
+    // (dt, dt x) of two channels are 16 bytes; those of an item's channels 0 and 1, of all items of the row, come first, then those of channels
+    // 2 and 3, and so on, and y likewise by 16 or 8 bytes: so that neighbouring lanes access neighbouring 16 bytes.
+    static constexpr int PS = 2 * CT + (2 * CT % 32 == 0 && ROWI < 8 ? 16 : 0), YV = VE < 4 ? VE : 4, YS = CT + 8;
+    __host__ __device__ static constexpr int p_at(int ch) { return (ch % VE / 2 * ROWI + ch / VE) * 4 + ch % 2 * 2; }
+    __host__ __device__ static constexpr int y_at(int ch) { return (ch % VE / YV * ROWI + ch / VE) * YV + ch % YV; }
+    static_assert(TB % TS == 0 && SUMS % LN == 0 && W * LN == 32 * CC && CT % VE == 0, "");
+    static constexpr int BC = sizeof(T) == 2 ? 1 : 2;        // words of (b, c): packed bf16 halves, or one each
     struct Shared {
-        alignas(16) T b[2][TB * S], c[2][TB * S];
-        alignas(16) float p[TB * PS];                        // (dt, dt x) of each row and channel
-        alignas(16) float y[TB * YS];
+        alignas(16) T x[kRing][TB * CT], dt[kRing][TB * CT], z[kRing][TB * CT], b[kRing][TB * S], c[kRing][TB * S];
+        alignas(16) float p[2][TB * PS];                 // (dt, dt x) of each row and channel
+        alignas(16) uint32_t bc[2][BC][TB * S];
+        alignas(16) float y[2][TB * YS];
+        alignas(16) float bias[CT], skip[CT];
+        int4 table[kSelfSort];
     };
 };
 
-constexpr int kWarps = 4;
-
-// ALIGNED: rows of x, dt, z and out, and the channels of a group, come in whole vectors of VE values.
+// ALIGNED: rows of x, dt, z and out, and the channels of a group, come in whole vectors of VE values, rows of b and c in whole 8 bytes.
 template <typename T, typename F, bool ALIGNED>
-__global__ void __launch_bounds__(32 * kWarps) selective_scan_kernel(const ScanArgs a, const uint32_t tiles, const uint32_t ctas)
+__global__ void __launch_bounds__(kThreads, 3) selective_scan_kernel(const ScanArgs a, const uint32_t tiles)
 {
-    constexpr int S = F::S, SS = F::SS, CC = F::CC, LN = F::LN, W = F::W, VE = F::VE, TB = F::TB, TS = F::TS;
+    constexpr int S = F::S, SS = F::SS, CC = F::CC, LN = F::LN, W = F::W, CT = F::CT, VE = F::VE, TB = F::TB, TS = F::TS;
     extern __shared__ __align__(16) unsigned char raw[];
-    __shared__ int4 table[kSelfSort];
+    typename F::Shared& sh = *reinterpret_cast<typename F::Shared*>(raw);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    typename F::Shared& sh = reinterpret_cast<typename F::Shared*>(raw)[warp];
 
-    allow_successor();
     wait_for_predecessor();
-    const uint32_t place = blockIdx.x / ctas, tile = (blockIdx.x - place * ctas) * kWarps + warp;
+    const uint32_t place = blockIdx.x / tiles, tile = blockIdx.x - place * tiles;
     int4 req;                                                // (first row, end row, request)
     if (a.num_seqs > 1 && a.num_seqs <= kSelfSort) {         // longest first; more requests than that fill the GPU in any order
-        sort_requests(a.cu, a.num_seqs, table, warp, kWarps, lane);
+        sort_requests(a.cu, a.num_seqs, sh.table, warp, kCompute + kHelpers, lane);
         __syncthreads();
-        req = table[place];
+        req = sh.table[place];
     } else {
         req = make_int4(a.cu[place], a.cu[place + 1], (int)place, 0);
     }
-    if (tile >= tiles) return;
     req.y = (int)min((int64_t)req.y, a.total_tokens);
     // tiles do not cross groups: b and c are one group's
-    const int each = a.channels / a.groups, per = (each + W - 1) / W, group = tile / per, first = group * each + (tile - group * per) * W;
+    const int each = a.channels / a.groups, per = (each + CT - 1) / CT, group = tile / per, first = group * each + (tile - group * per) * CT;
     const int limit = (group + 1) * each;
+    const int blocks = req.x < req.y ? (req.y - req.x + TB - 1) / TB : 0;
 
-    // lane = (channels, states)
-    const int sub = lane / LN, ln = lane % LN;
+    if (warp >= kCompute) {
+        const int id = threadIdx.x - 32 * kCompute;
+        // dt_bias and d of the tile's channels
+        for (int c = id; c < CT; c += 32 * kHelpers) {
+            sh.bias[c] = a.dt_bias && first + c < limit ? a.dt_bias[first + c] : 0.f;
+            sh.skip[c] = a.d && first + c < limit ? a.d[first + c] : 0.f;
+        }
+        // A helper's share of a block: ITEMS rows' pieces of VE channels (piece k is in row r0 + k RSTEP), and vectors of 8 bytes of b and c.  It
+        // copies what it reads itself later: no barrier in between.
+        constexpr int RSTEP = 32 * kHelpers / F::ROWI;
+        static_assert(32 * kHelpers % F::ROWI == 0, "a helper keeps its channels");
+        const int r0 = id / F::ROWI, ch = id % F::ROWI * VE;
+        constexpr int V8 = 8 / sizeof(T), BCI = TB * S / V8, BPT = (BCI + 32 * kHelpers - 1) / (32 * kHelpers), BSTEP = 32 * kHelpers / (S / V8);
+        static_assert(32 * kHelpers % (S / V8) == 0, "");
+        const int b0 = id / (S / V8), bs = id % (S / V8) * V8;
+        auto mine = [&](int k) { return F::ITEMS % (32 * kHelpers) == 0 || id + k * 32 * kHelpers < F::ITEMS; };
+        auto mine_bc = [&](int k) { return BCI % (32 * kHelpers) == 0 || id + k * 32 * kHelpers < BCI; };
+        const T* xp = static_cast<const T*>(a.x) + (int64_t)(req.x + r0) * a.x_stride + first + ch;      // of the block that is copied next
+        const T* dp = static_cast<const T*>(a.dt) + (int64_t)(req.x + r0) * a.dt_stride + first + ch;
+        const T* zp = static_cast<const T*>(a.z) + (int64_t)(req.x + r0) * a.z_stride + first + ch;
+        const T* bp = static_cast<const T*>(a.b) + (int64_t)(req.x + b0) * a.b_stride + group * S + bs;
+        const T* cp = static_cast<const T*>(a.c) + (int64_t)(req.x + b0) * a.c_stride + group * S + bs;
+        T* op = static_cast<T*>(a.out) + (int64_t)(req.x + r0) * a.out_stride + first + ch;              // of the block that is finished next
+        const bool real = first + ch < limit;
+        auto copy = [&](const T* src, T* dst) {
+            if (ALIGNED) {
+                constexpr int B = VE * sizeof(T) > 16 ? 16 : VE * sizeof(T);
+#pragma unroll
+                for (int v = 0; v < VE; v += B / sizeof(T)) copy_async<B>(dst + v, src + v);
+            } else {
+#pragma unroll
+                for (int v = 0; v < VE; ++v) dst[v] = first + ch + v < limit ? src[v] : round_to<T>(0.f);
+            }
+        };
+        auto issue = [&](int block) {
+            const int left = req.y - req.x - block * TB, slot = block % kRing;
+#pragma unroll
+            for (int k = 0; k < F::IPT; ++k) {
+                if (mine(k) && real && r0 + k * RSTEP < left) {
+                    const int at = (r0 + k * RSTEP) * CT + ch;
+                    copy(xp + k * RSTEP * a.x_stride, &sh.x[slot][at]);
+                    copy(dp + k * RSTEP * a.dt_stride, &sh.dt[slot][at]);
+                    if (a.z) copy(zp + k * RSTEP * a.z_stride, &sh.z[slot][at]);
+                }
+            }
+            xp += TB * a.x_stride; dp += TB * a.dt_stride; zp += TB * a.z_stride;
+#pragma unroll
+            for (int k = 0; k < BPT; ++k) {
+                if (mine_bc(k) && b0 + k * BSTEP < left) {
+                    const int at = (id + k * 32 * kHelpers) * V8;
+                    const T *b = bp + k * BSTEP * a.b_stride, *c = cp + k * BSTEP * a.c_stride;
+                    if (ALIGNED) {
+                        copy_async<8>(&sh.b[slot][at], b);
+                        copy_async<8>(&sh.c[slot][at], c);
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < V8; ++v) { sh.b[slot][at + v] = b[v]; sh.c[slot][at + v] = c[v]; }
+                    }
+                }
+            }
+            bp += TB * a.b_stride; cp += TB * a.c_stride;
+        };
+        auto commit = []() { asm volatile("cp.async.commit_group;" ::: "memory"); };
+        // (dt, dt x) and (b, c) of a block.  Rows past the request's end become zeros, whatever lies there: the state and the sums of the
+        // rows before do not see them.
+        auto prepare = [&](int block) {
+            const int slot = block % kRing, buf = block & 1, left = req.y - req.x - block * TB;
+            Pack<T, V8> b[BPT], c[BPT];
+#pragma unroll
+            for (int k = 0; k < BPT; ++k) {
+                if (!mine_bc(k)) break;
+                b[k] = *reinterpret_cast<const Pack<T, V8>*>(&sh.b[slot][(id + k * 32 * kHelpers) * V8]);
+                c[k] = *reinterpret_cast<const Pack<T, V8>*>(&sh.c[slot][(id + k * 32 * kHelpers) * V8]);
+            }
+#pragma unroll
+            for (int k = 0; k < F::IPT; ++k) {
+                if (!mine(k)) break;
+                const int r = r0 + k * RSTEP, at = r * CT + ch;
+                const Pack<T, VE> x = *reinterpret_cast<const Pack<T, VE>*>(&sh.x[slot][at]), dt = *reinterpret_cast<const Pack<T, VE>*>(&sh.dt[slot][at]);
+#pragma unroll
+                for (int v = 0; v < VE; v += 2) {
+                    F2 d = add(pair_at(dt, v), *reinterpret_cast<const F2*>(&sh.bias[ch + v]));
+                    if (a.softplus) d = softplus_of(d);
+                    const float2 dv = parts(d), dx = parts(mul(d, pair_at(x, v)));
+                    float4 q = make_float4(dv.x, dx.x, dv.y, dx.y);
+                    if (r >= left) q = make_float4(0.f, 0.f, 0.f, 0.f);
+                    *reinterpret_cast<float4*>(&sh.p[buf][r * F::PS + F::p_at(ch) + v / 2 * F::ROWI * 4]) = q;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < BPT; ++k) {
+                if (!mine_bc(k)) break;
+                const int at = (id + k * 32 * kHelpers) * V8;
+                Pack<uint32_t, V8> lo, hi;
+#pragma unroll
+                for (int v = 0; v < V8; ++v) {
+                    if constexpr (sizeof(T) == 2) lo.v[v] = (uint32_t)__bfloat16_as_ushort(b[k].v[v]) | (uint32_t)__bfloat16_as_ushort(c[k].v[v]) << 16;
+                    else { lo.v[v] = __float_as_uint(b[k].v[v]); hi.v[v] = __float_as_uint(c[k].v[v]); }
+                }
+                if (b0 + k * BSTEP >= left) lo = hi = {};
+                *reinterpret_cast<Pack<uint32_t, V8>*>(&sh.bc[buf][0][at]) = lo;
+                if (sizeof(T) == 4) *reinterpret_cast<Pack<uint32_t, V8>*>(&sh.bc[buf][F::BC - 1][at]) = hi;
+            }
+        };
+        auto finish = [&](int block) {
+            const int slot = block % kRing, buf = block & 1, left = req.y - req.x - block * TB;
+#pragma unroll
+            for (int k = 0; k < F::IPT; ++k) {
+                const int r = r0 + k * RSTEP, at = r * CT + ch;
+                if (!mine(k) || !real || r >= left) break;
+                const Pack<T, VE> x = *reinterpret_cast<const Pack<T, VE>*>(&sh.x[slot][at]);
+                Pack<T, VE> z, o;
+                if (a.z) z = *reinterpret_cast<const Pack<T, VE>*>(&sh.z[slot][at]);
+#pragma unroll
+                for (int u = 0; u < VE; u += F::YV) {
+                    const Pack<float, F::YV> y = *reinterpret_cast<const Pack<float, F::YV>*>(&sh.y[buf][r * F::YS + F::y_at(ch) + u * F::ROWI]);
+#pragma unroll
+                    for (int v = 0; v < F::YV; v += 2) {
+                        F2 w = fma(*reinterpret_cast<const F2*>(&sh.skip[ch + u + v]), pair_at(x, u + v), pair_at(y, v));
+                        if (a.z) w = mul(w, silu_of(pair_at(z, u + v)));
+                        const float2 f = parts(w);
+                        o.v[u + v] = round_to<T>(f.x); o.v[u + v + 1] = round_to<T>(f.y);
+                    }
+                }
+                T* dst = op + k * RSTEP * a.out_stride;
+                if (ALIGNED) {
+                    *reinterpret_cast<Pack<T, VE>*>(dst) = o;
+                } else {
+#pragma unroll
+                    for (int v = 0; v < VE; ++v)
+                        if (first + ch + v < limit) dst[v] = o.v[v];
+                }
+            }
+            op += TB * a.out_stride;
+        };
+        for (int i = 0; i < kRing - 1; ++i) {
+            if (i < blocks) issue(i);
+            commit();
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kHelpers) : "memory");     // (bias and skip)
+        if (blocks > 0) prepare(0);
+        __syncthreads();
+        for (int i = 0; i < blocks; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 3) : "memory");
+            if (i + 1 < blocks) prepare(i + 1);
+            if (i > 0) finish(i - 1);
+            if (i + kRing - 1 < blocks) issue(i + kRing - 1);                // (in the ring's place of block i - 1, which is done)
+            commit();
+            __syncthreads();
+        }
+        allow_successor();
+        if (blocks > 0) finish(blocks - 1);
+        return;
+    }
+
+    const int sub = lane / LN, ln = lane % LN, ch0 = warp * W + sub * CC;
     float h[CC][SS], a2[CC][SS];
     const int from = a.init_state ? slot_of(a.init_slots, req.z, a.num_init, a.status_word) : -1;
 #pragma unroll
     for (int c = 0; c < CC; ++c) {
-        const int ch = first + sub * CC + c;
+        const int ch = first + ch0 + c;
 #pragma unroll
         for (int s = 0; s < SS; ++s) h[c][s] = a2[c][s] = 0.f;
         if (ch < limit) {
@@ -141,109 +314,47 @@ __global__ void __launch_bounds__(32 * kWarps) selective_scan_kernel(const ScanA
 #pragma unroll
         for (int s = 0; s < SS; ++s) a2[c][s] *= kLog2e;
     }
-
-    // lane = (row, VE channels)
-    const int irow = lane / (W / VE), ich = (lane % (W / VE)) * VE, ch0 = first + ich;
-    float bias[VE], skip[VE];
+    __syncthreads();
+    for (int block = 0; block < blocks; ++block) {
+        const int buf = block & 1;
+        const float* ps = &sh.p[buf][F::p_at(ch0)];
+        const uint32_t *b0 = &sh.bc[buf][0][ln * SS], *b1 = &sh.bc[buf][F::BC - 1][ln * SS];
+        float* ys = &sh.y[buf][F::y_at(ch0)];                // (CC channels are neighbours there)
+        auto rows_of = [&](int t, float* sums) {
+            float b[SS], c[SS], p[2 * CC];
+            const Pack<uint32_t, SS> w = *reinterpret_cast<const Pack<uint32_t, SS>*>(b0 + t * S);
+            if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int v = 0; v < VE; ++v) {
-        bias[v] = a.dt_bias && ch0 + v < limit ? a.dt_bias[ch0 + v] : 0.f;
-        skip[v] = a.d && ch0 + v < limit ? a.d[ch0 + v] : 0.f;
-    }
-    Pack<T, VE> xn, dn, zn;
-    auto fetch = [&](const void* base, int64_t stride, int t, Pack<T, VE>& p) {
-        const T* src = static_cast<const T*>(base) + (int64_t)(t + irow) * stride + ch0;
-        if (ALIGNED && t + irow < req.y && ch0 < limit) {
-            p = *reinterpret_cast<const Pack<T, VE>*>(src);
-        } else {
+                for (int s = 0; s < SS; ++s) { b[s] = __uint_as_float(w.v[s] << 16); c[s] = __uint_as_float(w.v[s] & 0xffff0000u); }
+            } else {
+                const Pack<uint32_t, SS> w1 = *reinterpret_cast<const Pack<uint32_t, SS>*>(b1 + t * S);
 #pragma unroll
-            for (int v = 0; v < VE; ++v) p.v[v] = !ALIGNED && t + irow < req.y && ch0 + v < limit ? src[v] : round_to<T>(0.f);
-        }
-    };
-    // rows past the request's end are zeros: whatever lies there, the state and the sums of the rows before do not see it
-    auto stage = [&](const void* base, int64_t stride, int t, T* dst) {
-        const T* src = static_cast<const T*>(base) + (int64_t)group * S;
-        const uintptr_t al = (uintptr_t)src | (uintptr_t)(stride * (int64_t)sizeof(T));
-        constexpr int V16 = 16 / sizeof(T), V4 = 4 / sizeof(T);
-        if ((al & 15) == 0) {
-            for (int i = lane; i < TB * S / V16; i += 32) {
-                const int r = i / (S / V16), s = i % (S / V16) * V16;
-                const bool there = t + r < req.y;
-                copy_async<16>(dst + r * S + s, there ? src + (int64_t)(t + r) * stride + s : src, there);
+                for (int s = 0; s < SS; ++s) { b[s] = __uint_as_float(w.v[s]); c[s] = __uint_as_float(w1.v[s]); }
             }
-        } else if ((al & 3) == 0) {
-            for (int i = lane; i < TB * S / V4; i += 32) {
-                const int r = i / (S / V4), s = i % (S / V4) * V4;
-                const bool there = t + r < req.y;
-                copy_async<4>(dst + r * S + s, there ? src + (int64_t)(t + r) * stride + s : src, there);
-            }
-        } else {
-            for (int i = lane; i < TB * S; i += 32) {
-                const int r = i / S, s = i % S;
-                dst[i] = t + r < req.y ? src[(int64_t)(t + r) * stride + s] : round_to<T>(0.f);
-            }
-        }
-    };
-    auto fetch_all = [&](int t, int buf) {
-        fetch(a.x, a.x_stride, t, xn);
-        fetch(a.dt, a.dt_stride, t, dn);
-        if (a.z) fetch(a.z, a.z_stride, t, zn);
-        stage(a.b, a.b_stride, t, sh.b[buf]);
-        stage(a.c, a.c_stride, t, sh.c[buf]);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-
-    if (req.x < req.y) fetch_all(req.x, 0);
-    int buf = 0;
-    for (int t0 = req.x; t0 < req.y; t0 += TB, buf ^= 1) {
-        const Pack<T, VE> x = xn, z = zn;
-        const bool there = t0 + irow < req.y;
+            load_values<float, 2 * CC>(ps + t * F::PS, p);
 #pragma unroll
-        for (int v = 0; v < VE; ++v) {
-            float dt = widen<T>(dn.v[v]) + bias[v];
-            if (a.softplus) dt = softplus_of(dt);
-            if (!there) dt = 0.f;
-            *reinterpret_cast<float2*>(&sh.p[irow * F::PS + 2 * (ich + v)]) = make_float2(dt, dt * widen<T>(x.v[v]));
-        }
-        if (t0 + TB < req.y) {
-            fetch_all(t0 + TB, buf ^ 1);
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-        } else {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-        }
-        __syncwarp();
-
-#pragma unroll 1
-        for (int t = 0; t < TB; t += TS) {
-            float sums[F::SUMS];
+            for (int k = 0; k < CC; ++k) {
+                const float dt = p[2 * k], dx = p[2 * k + 1];
+                if constexpr (SS == 1) {
+                    h[k][0] = fmaf(ex2(dt * a2[k][0]), h[k][0], dx * b[0]);
+                    sums[k] = h[k][0] * c[0];
+                } else {
+                    F2 acc;
 #pragma unroll
-            for (int i = 0; i < TS; ++i) {
-                float b[SS], c[SS], p[2 * CC];
-                load_values<T, SS>(&sh.b[buf][(t + i) * S + ln * SS], b);
-                load_values<T, SS>(&sh.c[buf][(t + i) * S + ln * SS], c);
-                load_values<float, 2 * CC>(&sh.p[(t + i) * F::PS + sub * CC * 2], p);
-#pragma unroll
-                for (int k = 0; k < CC; ++k) {
-                    const float dt = p[2 * k], dx = p[2 * k + 1];
-                    if constexpr (SS == 1) {
-                        h[k][0] = fmaf(ex2(dt * a2[k][0]), h[k][0], dx * b[0]);
-                        sums[i * CC + k] = h[k][0] * c[0];
-                    } else {
-                        F2 acc;
-#pragma unroll
-                        for (int s = 0; s < SS; s += 2) {
-                            const float2 e = parts(mul(pair(dt, dt), pair(a2[k][s], a2[k][s + 1])));
-                            const F2 hn = fma(pair(ex2(e.x), ex2(e.y)), pair(h[k][s], h[k][s + 1]), mul(pair(dx, dx), pair(b[s], b[s + 1])));
-                            const float2 hv = parts(hn);
-                            h[k][s] = hv.x; h[k][s + 1] = hv.y;
-                            acc = s ? fma(hn, pair(c[s], c[s + 1]), acc) : mul(hn, pair(c[s], c[s + 1]));
-                        }
-                        const float2 r = parts(acc);
-                        sums[i * CC + k] = r.x + r.y;
+                    for (int s = 0; s < SS; s += 2) {
+                        const float2 e = parts(mul(pair(dt, dt), pair(a2[k][s], a2[k][s + 1])));
+                        const F2 hn = fma(pair(ex2(e.x), ex2(e.y)), pair(h[k][s], h[k][s + 1]), mul(pair(dx, dx), pair(b[s], b[s + 1])));
+                        const float2 hv = parts(hn);
+                        h[k][s] = hv.x; h[k][s + 1] = hv.y;
+                        acc = s ? fma(hn, pair(c[s], c[s + 1]), acc) : mul(hn, pair(c[s], c[s + 1]));
                     }
+                    const float2 r = parts(acc);
+                    sums[k] = r.x + r.y;
                 }
             }
-            // sum over LN lanes: each exchange halves what a lane is responsible for; lane ln ends with sums ln MINE ...
+        };
+        // sum over LN lanes: each exchange halves what a lane is responsible for; lane ln ends with sums ln MINE ...
+        auto reduce = [&](float (&sums)[F::SUMS]) {
 #pragma unroll
             for (int m = LN / 2, n = F::SUMS / 2; m >= 1; m /= 2, n /= 2) {
                 const bool up = ln & m;
@@ -255,36 +366,51 @@ __global__ void __launch_bounds__(32 * kWarps) selective_scan_kernel(const ScanA
                     }
                 }
             }
+        };
+        auto store = [&](int t, const float (&sums)[F::SUMS]) {
 #pragma unroll
             for (int i = 0; i < F::MINE; ++i) {
                 const int j = ln * F::MINE + i;
-                sh.y[(t + j / CC) * F::YS + sub * CC + j % CC] = sums[i];
+                ys[(t + j / CC) * F::YS + j % CC] = sums[i];
+            }
+        };
+        const int left = req.y - req.x - block * TB;
+        if (left < TB) {                                     // the last block: no more rows than there are
+#pragma unroll 1
+            for (int t = 0; t < left; t += TS) {
+                float sums[F::SUMS];
+#pragma unroll
+                for (int i = 0; i < TS; ++i) rows_of(t + i, &sums[i * CC]);
+                reduce(sums);
+                store(t, sums);
+            }
+        } else {
+            // the sums of TS rows are exchanged and stored while the next TS rows are computed: their loads come first, as the
+            // compiler cannot move them across the stores
+            float before[F::SUMS];
+#pragma unroll
+            for (int t = 0; t <= TB; t += TS) {
+                float sums[F::SUMS];
+                if (t < TB)
+#pragma unroll
+                    for (int i = 0; i < TS; ++i) rows_of(t + i, &sums[i * CC]);
+                if (t > 0) {
+                    reduce(before);
+                    store(t - TS, before);
+                }
+#pragma unroll
+                for (int i = 0; i < F::SUMS; ++i) before[i] = sums[i];
             }
         }
-        __syncwarp();
-
-        Pack<T, VE> o;
-#pragma unroll
-        for (int v = 0; v < VE; ++v) {
-            float y = fmaf(skip[v], widen<T>(x.v[v]), sh.y[irow * F::YS + ich + v]);
-            if (a.z) y *= silu_of(widen<T>(z.v[v]));
-            o.v[v] = round_to<T>(y);
-        }
-        T* dst = static_cast<T*>(a.out) + (int64_t)(t0 + irow) * a.out_stride + ch0;
-        if (ALIGNED) {
-            if (there && ch0 < limit) *reinterpret_cast<Pack<T, VE>*>(dst) = o;
-        } else {
-#pragma unroll
-            for (int v = 0; v < VE; ++v)
-                if (there && ch0 + v < limit) dst[v] = o.v[v];
-        }
+        __syncthreads();
     }
 
+    allow_successor();                                       // (earlier, the next call's CTAs crowd the SMs that are free already)
     const int to = a.out_state ? slot_of(a.out_slots, req.z, a.num_out, a.status_word) : -1;
     if (to < 0) return;
 #pragma unroll
     for (int c = 0; c < CC; ++c) {
-        const int ch = first + sub * CC + c;
+        const int ch = first + ch0 + c;
         if (ch >= limit) continue;
         Pack<float, SS> q;
 #pragma unroll
@@ -296,28 +422,34 @@ __global__ void __launch_bounds__(32 * kWarps) selective_scan_kernel(const ScanA
 template <typename T, typename F> cudaError_t launch_form(const ScanArgs& a, cudaStream_t stream)
 {
     const int each = a.channels / a.groups;
-    const uint32_t tiles = (uint32_t)a.groups * ((each + F::W - 1) / F::W), ctas = (tiles + kWarps - 1) / kWarps;
-    const uint64_t grid = (uint64_t)a.num_seqs * ctas;
+    const uint32_t tiles = (uint32_t)a.groups * ((each + F::CT - 1) / F::CT);
+    const uint64_t grid = (uint64_t)a.num_seqs * tiles;
     if (grid > 0x7fffffffull) return cudaErrorNotSupported;
     const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.dt | (uintptr_t)a.z | (uintptr_t)a.out |
                           (uintptr_t)((a.x_stride | a.dt_stride | (a.z ? a.z_stride : 0) | a.out_stride) * (int64_t)sizeof(T));
-    const bool aligned = all % alignof(Pack<T, F::VE>) == 0 && each % F::VE == 0;
-    constexpr size_t smem = kWarps * sizeof(typename F::Shared);
+    const uintptr_t bc = (uintptr_t)a.b | (uintptr_t)a.c | (uintptr_t)((a.b_stride | a.c_stride) * (int64_t)sizeof(T));
+    const bool aligned = all % alignof(Pack<T, F::VE>) == 0 && bc % 8 == 0 && each % F::VE == 0;
+    constexpr size_t smem = sizeof(typename F::Shared);
     auto kernel = aligned ? selective_scan_kernel<T, F, true> : selective_scan_kernel<T, F, false>;
-    if (smem > 40 * 1024) {                                  // (48 KB with the table of requests go without asking)
+    if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    return launch_kernel(kernel, (unsigned)grid, 32 * kWarps, smem, stream, 1, a, tiles, ctas);
+    return launch_kernel(kernel, (unsigned)grid, kThreads, smem, stream, 1, a, tiles);
 }
 
-// Lanes per state: the fewer states a lane holds the more warps there are, and the more a state costs.
+// How many states a lane holds.  With fewer there are more warps, and each is sooner done with a row; with more, what is done once per lane
+// and row (loads, sums) serves more of them.  By the states of the call per SM (requests x channels x states / 148); measured at 16
+// states, bf16, us with one / two / four states a lane: one request of 1,638 tokens and 1,024 channels (111 per SM) 30 / 40 / 59; 2,048 channels
+// (221) 49 / 40 / 59; 4,096 channels (443) 92 / 64 / 60; eight hits of 4,096 channels (3,542) 582 / 379 / 303.  fp32 reads twice the
+// words of b and c per state: there four states are two of two channels each, which share them (eight hits 417 -> 375), from more states on
+// (4,096 channels 71 with two a lane, 83).  64 states are summed over 16 lanes: two channels a lane halve that (4,096 channels 205 -> 188).
 template <typename T, int S> cudaError_t launch_states(const ScanArgs& a, cudaStream_t stream)
 {
-    const int64_t all = (int64_t)a.num_seqs * a.channels * S;
-    if (all > 148 * 4 * 32 * 16) return launch_form<T, Form<S, 4, 4, T>>(a, stream);
-    if (all > 148 * 4 * 32) return launch_form<T, Form<S, 2, 2, T>>(a, stream);
-    return launch_form<T, Form<S, S == 64 ? 2 : 1, 1, T>>(a, stream);
+    const int64_t per_sm = (int64_t)a.num_seqs * a.channels * S / 148;
+    if (S < 64 && per_sm <= 160) return launch_form<T, Form<S, S < 64 ? 1 : 2, 1, T>>(a, stream);
+    if (per_sm <= (sizeof(T) == 2 ? 320 : 700)) return launch_form<T, Form<S, 2, 1, T>>(a, stream);
+    return launch_form<T, Form<S, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2 && S < 64 ? 1 : 2, T>>(a, stream);
 }
 
 template <typename T> cudaError_t launch_type(const ScanArgs& a, int states, cudaStream_t stream)

@@ -199,10 +199,10 @@ cudaError_t launch(const ConvArgs& a, bool step, cudaStream_t stream)
 template <typename T>
 cudaError_t launch_width(const ConvArgs& a, int width, bool step, cudaStream_t stream)
 {
-    constexpr int VEC = 16 / sizeof(T);
+    constexpr int VEC = 4;
     const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.weight | (uintptr_t)a.bias | (uintptr_t)a.init_state | (uintptr_t)a.out |
                           (uintptr_t)a.out_state | (uintptr_t)((a.x_stride | a.out_stride) * (int64_t)sizeof(T));
-    const bool vec = (all & 15) == 0 && a.channels % VEC == 0;
+    const bool vec = (all & (VEC * sizeof(T) - 1)) == 0 && a.channels % VEC == 0;
     switch (width) {
         case 2: return vec ? launch<T, 2, VEC>(a, step, stream) : launch<T, 2, 1>(a, step, stream);
         case 3: return vec ? launch<T, 3, VEC>(a, step, stream) : launch<T, 3, 1>(a, step, stream);
