@@ -12,7 +12,7 @@ namespace cg = cooperative_groups;
 namespace gdn {
 namespace {
 
-constexpr int kCluster = 8, kThreads = 1024, kTeam = kCluster * kThreads;
+constexpr int kCluster = 8, kThreads = 1024, kTeam = kCluster * kThreads, kChunk = 256;
 constexpr int64_t kPiece = 4096;       // bytes that a warp moves at a time
 constexpr int kPoolsPerLaunch = 64;
 
@@ -141,27 +141,39 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) for
         a.plan.need[i] = ok ? need : -1;
     }
     cluster.sync();
-    const uint32_t entries = (uint32_t)a.count * W;  // (below 2^31)
-    for (uint32_t e = id; e < entries; e += kTeam) {
-        const int i = e / (uint32_t)W, j = e - i * W, need = __ldcg(&a.plan.need[i]);
-        if (j >= need) continue;
-        const int page = a.tables[(int64_t)a.parents[i] * W + j];
-        if (page < 0 || page >= a.num_pages) a.plan.need[i] = -1;            // (others may read either: the fork is left out by then)
+    // a warp takes kChunk entries of a fork's row at a time, all of them on their way at once
+    const uint32_t chunks = (W + kChunk - 1) / kChunk, items = (uint32_t)a.count * chunks, lane = tid % 32;
+    for (uint32_t e = id / 32; e < items; e += kTeam / 32) {
+        const int i = e / chunks, j0 = (e - i * chunks) * kChunk + lane, need = __ldcg(&a.plan.need[i]);
+        const int32_t* row = a.tables + (int64_t)(need > 0 ? a.parents[i] : 0) * W;
+        int page[kChunk / 32];
+#pragma unroll
+        for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < need ? row[j0 + 32 * u] : 0;
+        bool bad = false;
+#pragma unroll
+        for (int u = 0; u < kChunk / 32; ++u) bad |= page[u] < 0 || page[u] >= a.num_pages;
+        if (bad) a.plan.need[i] = -1;                // (others may read either: the fork is left out by then)
     }
     cluster.sync();
-    for (uint32_t e = id; e < entries; e += kTeam) {  // the children give back
-        const int i = e / (uint32_t)W, j = e - i * W;
+    for (uint32_t e = id / 32; e < items; e += kTeam / 32) {         // the children give back
+        const int i = e / chunks, j0 = (e - i * chunks) * kChunk + lane;
         if (__ldcg(&a.plan.need[i]) < 0) {
-            if (j == 0) report(a.status_word, GDN_ERR_BAD_INDEX);
+            if (j0 == 0) report(a.status_word, GDN_ERR_BAD_INDEX);
             continue;
         }
-        int32_t* at = a.tables + (int64_t)a.children[i] * W + j;
-        const int page = *at;
-        if (page == -1) continue;
-        *at = -1;
-        if (page < 0 || page >= a.num_pages) report(a.status_word, GDN_ERR_BAD_INDEX);
-        else if (atomicSub(&a.refcounts[page], 1) <= 0) {
-            atomicAdd(&a.refcounts[page], 1);
+        int32_t* row = a.tables + (int64_t)a.children[i] * W;
+        int page[kChunk / 32], held[kChunk / 32];
+#pragma unroll
+        for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < W ? row[j0 + 32 * u] : -1;
+#pragma unroll
+        for (int u = 0; u < kChunk / 32; ++u) {
+            if (page[u] != -1) row[j0 + 32 * u] = -1;
+            held[u] = page[u] >= 0 && page[u] < a.num_pages ? atomicSub(&a.refcounts[page[u]], 1) : page[u] == -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kChunk / 32; ++u) {
+            if (held[u] > 0) continue;               // (an entry that names no page, or a free one)
+            if (page[u] >= 0 && page[u] < a.num_pages) atomicAdd(&a.refcounts[page[u]], 1);
             report(a.status_word, GDN_ERR_BAD_INDEX);
         }
     }

@@ -34,6 +34,57 @@ constexpr float kLog2e = 1.4426950408889634f;
 // x sigmoid(x)
 __device__ __forceinline__ float silu_of(float x) { return x * rcp(1.f + ex2(-kLog2e * x)); }
 
+// ---- pairs of fp32 values in one register pair (add, multiply, fma on both at once)
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 pair(float a, float b)
+{
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 parts(F2 a)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul(F2 a, F2 b)
+{
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c)
+{
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 add(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 both(float a) { return pair(a, a); }
+__device__ __forceinline__ F2 silu_of(F2 x)
+{
+    const float2 e = parts(mul(x, both(-kLog2e))), s = parts(add(pair(ex2(e.x), ex2(e.y)), both(1.f)));
+    return mul(x, pair(rcp(s.x), rcp(s.y)));
+}
+
+// values v and v + 1 of a pack
+template <typename T, int N> __device__ __forceinline__ F2 pair_at(const Pack<T, N>& p, int v) { return pair(widen<T>(p.v[v]), widen<T>(p.v[v + 1])); }
+
+// asynchronous copies to shared memory
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+template <int B> __device__ __forceinline__ void copy_async(void* dst, const void* src)
+{
+    static_assert(B == 4 || B == 8 || B == 16, "");
+    if (B == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_addr(dst)), "l"(src), "n"(B) : "memory");
+}
+
 // slots[n] (no list: n) where the pool has it, else -1; a slot past the pool's end is reported
 __device__ __forceinline__ int slot_of(const int32_t* slots, int n, int num_slots, int32_t* status_word)
 {

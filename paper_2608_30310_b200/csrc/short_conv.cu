@@ -11,69 +11,77 @@
 namespace gdn {
 namespace {
 
-constexpr int kAhead = 8;              // rows loaded side by side
+constexpr int kRows = 4, kGroups = 4, kResident = 6;   // kResident: CTAs on an SM
+
+// VEC channels as pairs; a single channel is the first half of one
+template <int VEC> struct Values {
+    static constexpr int N = (VEC + 1) / 2;
+    F2 v[N];
+};
+template <typename T, int VEC> __device__ __forceinline__ Values<VEC> widened(const Pack<T, VEC>& p)
+{
+    Values<VEC> r;
+#pragma unroll
+    for (int i = 0; i < Values<VEC>::N; ++i) r.v[i] = pair(widen<T>(p.v[2 * i]), 2 * i + 1 < VEC ? widen<T>(p.v[2 * i + 1 < VEC ? 2 * i + 1 : 0]) : 0.f);
+    return r;
+}
 
 template <typename T, int K, int VEC>
 struct Window {
-    float w[K][VEC], bias[VEC], hist[K - 1][VEC];
+    static constexpr int N = Values<VEC>::N;
+    Values<VEC> w[K], bias, hist[K - 1];
     bool silu;
 
     __device__ __forceinline__ void load_weights(const ConvArgs& a, int c)
     {
         silu = a.silu;
-        Pack<T, VEC * K> p;
         const T* weight = static_cast<const T*>(a.weight) + (size_t)c * K;
+        Pack<T, VEC * K> p;
         if (VEC > 1) p = *reinterpret_cast<const Pack<T, VEC * K>*>(weight);
         else
 #pragma unroll
             for (int j = 0; j < K; ++j) p.v[j] = weight[j];
 #pragma unroll
-        for (int v = 0; v < VEC; ++v)
+        for (int j = 0; j < K; ++j) {
+            Pack<T, VEC> q;
 #pragma unroll
-            for (int j = 0; j < K; ++j) w[j][v] = widen<T>(p.v[v * K + j]);
-        if (a.bias) {
-            const Pack<T, VEC> q = *reinterpret_cast<const Pack<T, VEC>*>(static_cast<const T*>(a.bias) + c);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) bias[v] = widen<T>(q.v[v]);
-        } else {
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) bias[v] = 0.f;
+            for (int v = 0; v < VEC; ++v) q.v[v] = p.v[v * K + j];
+            w[j] = widened<T, VEC>(q);
         }
+        if (a.bias) bias = widened<T, VEC>(*reinterpret_cast<const Pack<T, VEC>*>(static_cast<const T*>(a.bias) + c));
+        else bias = {};
     }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) hist[j][v] = 0.f;
+        for (int j = 0; j < K - 1; ++j) hist[j] = {};
     }
-    __device__ __forceinline__ void set(int j, const Pack<T, VEC>& p)
-    {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) hist[j][v] = widen<T>(p.v[v]);
-    }
+    __device__ __forceinline__ void set(int j, const Pack<T, VEC>& p) { hist[j] = widened<T, VEC>(p); }
     // the next row in, its result out
     __device__ __forceinline__ Pack<T, VEC> step(const Pack<T, VEC>& p)
     {
+        const Values<VEC> x = widened<T, VEC>(p);
         Pack<T, VEC> out;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            const float x = widen<T>(p.v[v]);
-            float acc = bias[v];
+        for (int i = 0; i < N; ++i) {
+            F2 acc = bias.v[i];
 #pragma unroll
-            for (int j = 0; j < K - 1; ++j) acc = fmaf(w[j][v], hist[j][v], acc);
-            acc = fmaf(w[K - 1][v], x, acc);
-#pragma unroll
-            for (int j = 0; j < K - 2; ++j) hist[j][v] = hist[j + 1][v];
-            hist[K - 2][v] = x;
-            out.v[v] = round_to<T>(silu ? silu_of(acc) : acc);
+            for (int j = 0; j < K - 1; ++j) acc = fma(w[j].v[i], hist[j].v[i], acc);
+            acc = fma(w[K - 1].v[i], x.v[i], acc);
+            if (silu) acc = silu_of(acc);
+            const float2 r = parts(acc);
+            out.v[2 * i] = round_to<T>(r.x);
+            if (2 * i + 1 < VEC) out.v[2 * i + 1 < VEC ? 2 * i + 1 : 0] = round_to<T>(r.y);
         }
+#pragma unroll
+        for (int j = 0; j < K - 2; ++j) hist[j] = hist[j + 1];
+        hist[K - 2] = x;
         return out;
     }
 };
 
 template <typename T, int K, int VEC>
-__global__ void __launch_bounds__(128) short_conv_kernel(const ConvArgs a, const int rows, const uint32_t vectors, const uint32_t tiles)
+__global__ void __launch_bounds__(128, kResident) short_conv_kernel(const ConvArgs a, const int rows, const uint32_t vectors, const uint32_t tiles)
 {
     using P = Pack<T, VEC>;
     const uint32_t id = blockIdx.x * 128u + threadIdx.x, tile = id / vectors, c = (id - tile * vectors) * VEC;
@@ -91,15 +99,39 @@ __global__ void __launch_bounds__(128) short_conv_kernel(const ConvArgs a, const
     const T* init = a.init_state ? static_cast<const T*>(a.init_state) + c : nullptr;
     T* keep = a.out_state ? static_cast<T*>(a.out_state) + c : nullptr;
     auto row = [&](int t) { return *reinterpret_cast<const P*>(x + (int64_t)t * a.x_stride); };
+    // Groups of kRows rows are copied to shared memory kGroups - 1 ahead of the walk: registers for as many loads in flight would leave
+    // too few warps.  A thread reads what it copied itself; nothing waits for another.
+    __shared__ P ring[kGroups * kRows][128];
     auto walk = [&](int t, int end) {
-        for (; t < end; t += kAhead) {
-            P p[kAhead];
+        const T* from = x + (int64_t)t * a.x_stride;
+        T* to = out + (int64_t)t * a.out_stride;
+        const int rows_left = end - t, groups = (rows_left + kRows - 1) / kRows;
+        auto issue = [&](int g) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (t + i < end) p[i] = row(t + i);
+            for (int i = 0; i < kRows; ++i, from += a.x_stride)
+                if (g * kRows + i < rows_left) {
+                    P* dst = &ring[g % kGroups * kRows + i][threadIdx.x];
+                    if constexpr (sizeof(P) >= 4) copy_async<sizeof(P)>(dst, from);
+                    else *dst = *reinterpret_cast<const P*>(from);
+                }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int g = 0; g < kGroups - 1; ++g) issue(g);
+        for (int g = 0; g < groups; ++g) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kGroups - 2) : "memory");
+            P p[kRows];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (t + i < end) *reinterpret_cast<P*>(out + (int64_t)(t + i) * a.out_stride) = win.step(p[i]);
+            for (int i = 0; i < kRows; ++i) p[i] = ring[g % kGroups * kRows + i][threadIdx.x];
+            issue(g + kGroups - 1);
+            const int here = rows_left - g * kRows;
+            if (here >= kRows) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i, to += a.out_stride) *reinterpret_cast<P*>(to) = win.step(p[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRows - 1; ++i, to += a.out_stride)
+                    if (i < here) *reinterpret_cast<P*>(to) = win.step(p[i]);
+            }
         }
     };
 
@@ -188,9 +220,11 @@ cudaError_t launch(const ConvArgs& a, bool step, cudaStream_t stream)
         if (threads > 0xffffffffull - 128) return cudaErrorNotSupported;
         return launch_kernel(short_conv_step_kernel<T, K, VEC>, (unsigned)((threads + 127) / 128), 128, 0, stream, 1, a, vectors);
     }
-    // Rows per thread: the longest walk that still leaves every SM 512 threads.
-    int rows = 64;
-    while (rows > kAhead && (uint64_t)((a.total_tokens + rows - 1) / rows) * vectors < 148 * 512) rows /= 2;
+    // Rows per thread: two rounds of resident CTAs, but at least eight rows (four hits of 8,192 channels, 51 us at the copy rate: one round 69 us,
+    // two 66, four 68; 32 hits 357, 338, 334; 410 rows 5.9).
+    const int64_t threads_wanted = 2 * 148ll * kResident * 128;
+    int rows = (int)((a.total_tokens * (int64_t)vectors + threads_wanted - 1) / threads_wanted);
+    rows = rows < 8 ? 8 : (rows + kRows - 1) / kRows * kRows;
     const uint64_t tiles = a.total_tokens > 0 ? (uint64_t)(a.total_tokens + rows - 1) / rows : 1, threads = tiles * vectors;
     if (threads > 0xffffffffull - 128) return cudaErrorNotSupported;
     return launch_kernel(short_conv_kernel<T, K, VEC>, (unsigned)((threads + 127) / 128), 128, 0, stream, 1, a, rows, vectors, (uint32_t)tiles);
