@@ -335,9 +335,10 @@ GDN_API int32_t gdn_cache_copy(const gdn_cache_desc* desc, const int32_t* src, c
  * free one, which the child alone holds; the rest of the child's row is -1.  All children give back before any takes a page.
  * A child may be named once and may not be a parent in the same call; tokens fit the row; the parent holds pages for them.  A fork that
  * breaks this is left out, its child's row as it was (GDN_ERR_BAD_INDEX).  Too few free pages: the forks that get none, the last ones
- * that need one, leave their child's row empty (GDN_ERR_NO_PAGES).  At most GDN_CACHE_MAX_ROWS rows.
+ * that need one, leave their child's row empty (GDN_ERR_NO_PAGES).  At most GDN_CACHE_MAX_ROWS rows and GDN_CACHE_MAX_FORKS forks.
  */
 #define GDN_CACHE_MAX_ROWS 262144
+#define GDN_CACHE_MAX_FORKS 4096
 GDN_API int32_t gdn_cache_fork(const gdn_cache_desc* desc, int32_t* refcounts, int32_t* tables, const int32_t* parents,
                                const int32_t* children, const int32_t* tokens, int32_t count);
 

@@ -171,11 +171,11 @@ int32_t gdn_cache_fork(const gdn_cache_desc* d, int32_t* refcounts, int32_t* tab
     int32_t rc = check_cache(d, true, count, true);
     if (rc != GDN_OK) return rc;
     if (d->page_tokens <= 0) return GDN_ERR_INVALID_ARG;
-    if (d->num_rows > GDN_CACHE_MAX_ROWS) return GDN_ERR_UNSUPPORTED;
+    if (d->num_rows > GDN_CACHE_MAX_ROWS || count > GDN_CACHE_MAX_FORKS) return GDN_ERR_UNSUPPORTED;
     if (count == 0) return GDN_OK;
     if (!ints(refcounts) || !ints(tables) || !ints(parents) || !ints(children) || !ints(tokens)) return GDN_ERR_INVALID_ARG;
     if ((rc = check_workspace(d, count)) != GDN_OK) return rc;
-    return done(gdn::launch_cache_fork(d, refcounts, tables, parents, children, tokens, count), 1 + gdn::pool_launches(d));
+    return done(gdn::launch_cache_fork(d, refcounts, tables, parents, children, tokens, count), gdn::fork_launches(d, count));
 }
 
 int32_t gdn_cache_free(const gdn_cache_desc* d, int32_t* refcounts, int32_t* tables, const int32_t* rows, int32_t count)

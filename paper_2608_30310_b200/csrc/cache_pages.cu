@@ -1,7 +1,7 @@
 // Pages of a cache: copied, shared by forks, given back, brought to the front.
 //
-// The bookkeeping (which pages are free, which page moves where) is the work of one cluster of eight CTAs: it is a few prefix sums over
-// num_pages counts, whose steps need cluster barriers between them.  The kernel after it moves the pages with the whole GPU, in pieces of 4 KB
+// The bookkeeping (which pages are free, which page moves where) is the work of a single CTA or a cluster of eight: it is a few prefix sums over
+// num_pages counts, whose steps need barriers between them.  The kernel after it moves the pages with the whole GPU, in pieces of 4 KB
 // per warp, eight 16-byte loads in flight per lane; it is bound by HBM.  Nothing depends on the order in which threads run: free pages
 // are ranked by number, counts change by atomic integer additions.
 #include <cooperative_groups.h>
@@ -12,7 +12,7 @@ namespace cg = cooperative_groups;
 namespace gdn {
 namespace {
 
-constexpr int kCluster = 8, kThreads = 1024, kTeam = kCluster * kThreads, kChunk = 256;
+constexpr int kCluster = 8, kThreads = 1024, kChunk = 256;
 constexpr int64_t kPiece = 4096;       // bytes that a warp moves at a time
 constexpr int kPoolsPerLaunch = 64;
 
@@ -86,15 +86,15 @@ __device__ int scan_cta(int v, int* total, int* part)
     return before_warp + x - v;
 }
 
-// Each CTA's number to all CTAs: the sum over the CTAs before this one, and over all.
+// Each CTA's number to all CTAs of the cluster: the sum over the CTAs before this one, and over all.
 __device__ int scan_cluster(int mine, int* total, int* box)
 {
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank();
-    if (threadIdx.x < kCluster) cluster.map_shared_rank(box, threadIdx.x)[rank] = mine;
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    if (threadIdx.x < ctas) cluster.map_shared_rank(box, threadIdx.x)[rank] = mine;
     cluster.sync();
     int before = 0, all = 0;
-    for (int r = 0; r < kCluster; ++r) {
+    for (int r = 0; r < ctas; ++r) {
         before += r < rank ? box[r] : 0;
         all += box[r];
     }
@@ -115,74 +115,97 @@ struct ForkArgs {
     ForkPlan plan;
 };
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a)
+// kChunk entries of the child's row of fork i, from its entry j0 on (lanes 32 apart), given back
+__device__ __forceinline__ void give_back(const ForkArgs& a, int child, int j0)
 {
-    extern __shared__ uint32_t named[];              // rows that are children: once or more; more than once
-    __shared__ int part[32], box[kCluster];
+    int32_t* row = a.tables + (int64_t)child * a.row_pages;
+    int page[kChunk / 32], held[kChunk / 32];
+#pragma unroll
+    for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < a.row_pages ? row[j0 + 32 * u] : -1;
+#pragma unroll
+    for (int u = 0; u < kChunk / 32; ++u) {
+        if (page[u] != -1) row[j0 + 32 * u] = -1;
+        held[u] = page[u] >= 0 && page[u] < a.num_pages ? atomicSub(&a.refcounts[page[u]], 1) : page[u] == -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kChunk / 32; ++u) {
+        if (held[u] > 0) continue;                   // (an entry that names no page, or a free one)
+        if (page[u] >= 0 && page[u] < a.num_pages) atomicAdd(&a.refcounts[page[u]], 1);
+        report(a.status_word, GDN_ERR_BAD_INDEX);
+    }
+}
+
+// What a fork takes and whether it may (kCheck), the children's pages given back (kGiveBack), the free pages handed out (kTake).  Few entries: all
+// in one launch; many: the giving back is a kernel of its own between the two others, as its atomics want more SMs than a cluster has.
+constexpr int kCheck = 1, kGiveBack = 2, kTake = 4;
+
+__global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, const int steps)
+{
+    extern __shared__ int32_t forks[];               // [count] each: parent, child, pages that the child takes (the last one in part; -1: no
+    __shared__ int part[32], box[kCluster];          // fork), whole pages; then the rows that are children: once or more; more than once
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), tid = threadIdx.x, id = rank * kThreads + tid;
-    const int words = (a.num_rows + 31) / 32, W = a.row_pages;
-    uint32_t* twice = named + words;
-    for (int i = tid; i < 2 * words; i += kThreads) named[i] = 0;
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, lane = tid % 32, F = a.count, W = a.row_pages;
+    int32_t *parent = forks, *child = forks + F, *need = forks + 2 * F, *whole = forks + 3 * F;
+    uint32_t *named = reinterpret_cast<uint32_t*>(forks + 4 * F), *twice = named + (a.num_rows + 31) / 32;
+    if (steps & kCheck)
+        for (int i = tid; i < (a.num_rows + 31) / 32; i += kThreads) named[i] = twice[i] = 0;
+    cluster.sync();                                  // (all CTAs are there: they write to each other's memory)
     wait_for_predecessor();
-    __syncthreads();
-    for (int i = tid; i < a.count; i += kThreads) {
-        const int c = a.children[i];
-        if (c < 0 || c >= a.num_rows) continue;
-        const uint32_t bit = 1u << (c & 31);
-        if (atomicOr(&named[c >> 5], bit) & bit) atomicOr(&twice[c >> 5], bit);
-    }
-    __syncthreads();
-    auto has = [](const uint32_t* set, int r) { return (set[r >> 5] >> (r & 31)) & 1u; };
-    for (int i = id; i < a.count; i += kTeam) {      // pages that the child takes from its parent, the last one in part; -1: no fork
+    for (int i = tid; i < F; i += kThreads) {
         const int p = a.parents[i], c = a.children[i], n = a.tokens[i];
-        const int need = n < 0 ? -1 : n / a.page_tokens + (n % a.page_tokens > 0);
-        const bool ok = p >= 0 && p < a.num_rows && c >= 0 && c < a.num_rows && need >= 0 && need <= W && !has(twice, c) && !has(named, p);
-        a.plan.need[i] = ok ? need : -1;
-    }
-    cluster.sync();
-    // a warp takes kChunk entries of a fork's row at a time, all of them on their way at once
-    const uint32_t chunks = (W + kChunk - 1) / kChunk, items = (uint32_t)a.count * chunks, lane = tid % 32;
-    for (uint32_t e = id / 32; e < items; e += kTeam / 32) {
-        const int i = e / chunks, j0 = (e - i * chunks) * kChunk + lane, need = __ldcg(&a.plan.need[i]);
-        const int32_t* row = a.tables + (int64_t)(need > 0 ? a.parents[i] : 0) * W;
-        int page[kChunk / 32];
-#pragma unroll
-        for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < need ? row[j0 + 32 * u] : 0;
-        bool bad = false;
-#pragma unroll
-        for (int u = 0; u < kChunk / 32; ++u) bad |= page[u] < 0 || page[u] >= a.num_pages;
-        if (bad) a.plan.need[i] = -1;                // (others may read either: the fork is left out by then)
-    }
-    cluster.sync();
-    for (uint32_t e = id / 32; e < items; e += kTeam / 32) {         // the children give back
-        const int i = e / chunks, j0 = (e - i * chunks) * kChunk + lane;
-        if (__ldcg(&a.plan.need[i]) < 0) {
-            if (j0 == 0) report(a.status_word, GDN_ERR_BAD_INDEX);
-            continue;
-        }
-        int32_t* row = a.tables + (int64_t)a.children[i] * W;
-        int page[kChunk / 32], held[kChunk / 32];
-#pragma unroll
-        for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < W ? row[j0 + 32 * u] : -1;
-#pragma unroll
-        for (int u = 0; u < kChunk / 32; ++u) {
-            if (page[u] != -1) row[j0 + 32 * u] = -1;
-            held[u] = page[u] >= 0 && page[u] < a.num_pages ? atomicSub(&a.refcounts[page[u]], 1) : page[u] == -1;
-        }
-#pragma unroll
-        for (int u = 0; u < kChunk / 32; ++u) {
-            if (held[u] > 0) continue;               // (an entry that names no page, or a free one)
-            if (page[u] >= 0 && page[u] < a.num_pages) atomicAdd(&a.refcounts[page[u]], 1);
-            report(a.status_word, GDN_ERR_BAD_INDEX);
+        parent[i] = p;
+        child[i] = c;
+        whole[i] = n < 0 ? 0 : n / a.page_tokens;
+        if (steps & kCheck) {
+            need[i] = n < 0 ? -1 : whole[i] + (n % a.page_tokens > 0);
+            if (c < 0 || c >= a.num_rows) continue;
+            const uint32_t bit = 1u << (c & 31);
+            if (atomicOr(&named[c >> 5], bit) & bit) atomicOr(&twice[c >> 5], bit);
+        } else {
+            need[i] = a.plan.need[i];
         }
     }
-    cluster.sync();
+    __syncthreads();
+    const int chunks = (W + kChunk - 1) / kChunk, items = F * chunks, warps = ctas * (kThreads / 32), first = rank * (kThreads / 32) + tid / 32;
+    if (steps & kCheck) {
+        auto has = [](const uint32_t* set, int r) { return (set[r >> 5] >> (r & 31)) & 1u; };
+        for (int i = tid; i < F; i += kThreads) {
+            const int p = parent[i], c = child[i];
+            if (!(p >= 0 && p < a.num_rows && c >= 0 && c < a.num_rows && need[i] <= W && !has(twice, c) && !has(named, p))) need[i] = -1;
+        }
+        cluster.sync();
+        // a warp takes kChunk entries of a parent's row at a time, all of them on their way at once
+        for (int e = first; e < items; e += warps) {
+            const int i = e / chunks, j0 = (e - i * chunks) * kChunk + lane, n = need[i];
+            const int32_t* row = a.tables + (int64_t)(n > 0 ? parent[i] : 0) * W;
+            int page[kChunk / 32];
+#pragma unroll
+            for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < n ? row[j0 + 32 * u] : 0;
+            bool bad = false;
+#pragma unroll
+            for (int u = 0; u < kChunk / 32; ++u) bad |= page[u] < 0 || page[u] >= a.num_pages;
+            if (bad)                                 // (others may read either: the fork is left out by then)
+                for (int r = 0; r < ctas; ++r) *(volatile int32_t*)(cluster.map_shared_rank(need, r) + i) = -1;
+        }
+        cluster.sync();
+        for (int i = rank * kThreads + tid; i < F; i += ctas * kThreads) {
+            if (need[i] < 0) report(a.status_word, GDN_ERR_BAD_INDEX);
+            if (!(steps & kTake)) a.plan.need[i] = need[i];
+        }
+    }
+    if (steps & kGiveBack) {
+        for (int e = first; e < items; e += warps) {
+            const int i = e / chunks;
+            if (need[i] >= 0) give_back(a, child[i], (e - i * chunks) * kChunk + lane);
+        }
+        cluster.sync();
+    }
+    allow_successor();
+    if (!(steps & kTake)) return;
     // free pages, ranked by number: each CTA counts those of its share of the pages, then lists the first `wanted`
     int wanted = 0;
-    for (int i = tid; i - tid < a.count; i += kThreads)
-        wanted += __syncthreads_count(i < a.count && __ldcg(&a.plan.need[i]) > 0 && a.tokens[i] % a.page_tokens > 0);
-    const int slice = (a.num_pages + kCluster - 1) / kCluster, lo = min(rank * slice, a.num_pages), hi = min(lo + slice, a.num_pages);
+    for (int i = tid; i - tid < F; i += kThreads) wanted += __syncthreads_count(i < F && need[i] > whole[i]);
+    const int slice = (a.num_pages + ctas - 1) / ctas, lo = min(rank * slice, a.num_pages), hi = min(lo + slice, a.num_pages);
     int mine = 0, there, all_free;
     for (int p = lo + tid; p < hi; p += kThreads) mine += __ldcg(&a.refcounts[p]) <= 0;
     scan_cta(mine, &there, part);
@@ -195,28 +218,37 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) for
         before += there;
     }
     cluster.sync();
-    allow_successor();
     if (rank) return;
     int given = 0;
-    for (int i0 = 0; i0 < a.count; i0 += kThreads) {
+    for (int i0 = 0; i0 < F; i0 += kThreads) {
         const int i = i0 + tid;
-        const int need = i < a.count ? __ldcg(&a.plan.need[i]) : -1, n = i < a.count ? a.tokens[i] : 0;
-        const bool partial = need > 0 && n % a.page_tokens > 0;
+        const bool partial = i < F && need[i] > whole[i];
         int taken;
         const int at = given + scan_cta(partial, &taken, part);
         given += taken;
-        if (i >= a.count) continue;
-        int share = need < 0 ? 0 : n / a.page_tokens, src = -1, dst = -1;
+        if (i >= F) continue;
+        int share = need[i] < 0 ? 0 : whole[i], src = -1, dst = -1;
         if (partial && at < all_free) {
-            src = a.tables[(int64_t)a.parents[i] * W + share];
+            src = a.tables[(int64_t)parent[i] * W + share];
             dst = __ldcg(&a.plan.free[at]);
-            a.tables[(int64_t)a.children[i] * W + share] = dst;
+            a.tables[(int64_t)child[i] * W + share] = dst;
             a.refcounts[dst] = 1;
         } else if (partial) {
             share = 0;
             report(a.status_word, GDN_ERR_NO_PAGES);
         }
         a.plan.src[i] = src; a.plan.dst[i] = dst; a.plan.share[i] = share;
+    }
+}
+
+__global__ void __launch_bounds__(256) give_back_kernel(const ForkArgs a)
+{
+    allow_successor();
+    wait_for_predecessor();
+    const int chunks = (a.row_pages + kChunk - 1) / kChunk, items = a.count * chunks;
+    for (int e = (blockIdx.x * blockDim.x + threadIdx.x) / 32; e < items; e += gridDim.x * blockDim.x / 32) {
+        const int i = e / chunks;
+        if (a.plan.need[i] >= 0) give_back(a, a.children[i], (e - i * chunks) * kChunk + threadIdx.x % 32);
     }
 }
 
@@ -277,14 +309,14 @@ struct CompactArgs {
     CompactPlan plan;
 };
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads) compact_plan_kernel(const CompactArgs a)
+__global__ void __launch_bounds__(kThreads) compact_plan_kernel(const CompactArgs a)
 {
     __shared__ int part[32], box[kCluster];
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), tid = threadIdx.x, P = a.num_pages;
     cluster.sync();                                  // (all CTAs are there: they write to each other's memory)
     wait_for_predecessor();
-    const int slice = (P + kCluster - 1) / kCluster, lo = min(rank * slice, P), hi = min(lo + slice, P);
+    const int slice = (P + (int)cluster.num_blocks() - 1) / (int)cluster.num_blocks(), lo = min(rank * slice, P), hi = min(lo + slice, P);
     int mine = 0, there, all_free;
     for (int p = lo + tid; p < hi; p += kThreads) mine += a.refcounts[p] <= 0;
     scan_cta(mine, &there, part);
@@ -355,7 +387,13 @@ unsigned grid_for(uint64_t pieces, uint64_t entries)
     return (unsigned)(ctas < 1 ? 1 : ctas > 148 * 4 ? 148 * 4 : ctas);
 }
 
+// CTAs of a planning kernel: one where little is to be read, whose barriers cost least, else a cluster
+unsigned plan_ctas(int64_t pages, int64_t entries) { return pages <= 8192 && entries <= 8192 ? 1 : kCluster; }
+constexpr int64_t kFewEntries = 16384;
+
 }  // namespace
+
+int fork_launches(const gdn_cache_desc* d, int32_t count) { return ((int64_t)count * d->row_pages <= kFewEntries ? 1 : 3) + pool_launches(d); }
 
 int pool_launches(const gdn_cache_desc* d) { return d->num_pools > 0 ? (d->num_pools + kPoolsPerLaunch - 1) / kPoolsPerLaunch : 1; }
 
@@ -376,11 +414,19 @@ cudaError_t launch_cache_fork(const gdn_cache_desc* d, int32_t* refcounts, int32
     ForkArgs a = {refcounts, tables, parents, children, tokens, count, d->num_pages, d->num_rows, d->row_pages, d->page_tokens, d->status_word, {}};
     int32_t* w = (int32_t*)d->workspace;
     a.plan = {w, w + count, w + 2 * (int64_t)count, w + 3 * (int64_t)count, w + 4 * (int64_t)count};
-    const size_t smem = 2 * sizeof(uint32_t) * ((d->num_rows + 31) / 32);
+    const size_t smem = 4 * sizeof(int32_t) * (size_t)count + 2 * sizeof(uint32_t) * ((d->num_rows + 31) / 32);
     cudaStream_t stream = (cudaStream_t)d->stream;
     cudaError_t e = cudaSuccess;
     if (smem > 40 * 1024) e = cudaFuncSetAttribute(fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess) e = launch_kernel(fork_plan_kernel, kCluster, kThreads, smem, stream, 1, a);
+    const int64_t entries = (int64_t)count * d->row_pages;
+    const unsigned ctas = plan_ctas(d->num_pages, entries);
+    if (e == cudaSuccess && entries <= kFewEntries) {
+        e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a, kCheck | kGiveBack | kTake);
+    } else if (e == cudaSuccess) {
+        e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a, kCheck);
+        if (e == cudaSuccess) e = launch_kernel(give_back_kernel, grid_for(0, entries), 256, 0, stream, 1, a);
+        if (e == cudaSuccess) e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a, kTake);
+    }
     for (int i = 0; i < pool_launches(d) && e == cudaSuccess; ++i) {
         const Pools p = pools_from(d, i * kPoolsPerLaunch);
         e = launch_kernel(fork_kernel, grid_for((uint64_t)count * p.pieces[p.count], (uint64_t)count * d->row_pages), 256, 0, stream, 1, p, a, i == 0);
@@ -401,7 +447,8 @@ cudaError_t launch_cache_compact(const gdn_cache_desc* d, const int32_t* refcoun
     int32_t* w = (int32_t*)d->workspace;
     a.plan = {w, w + 64, w + 64 + (int64_t)d->num_pages, w + 64 + 2 * (int64_t)d->num_pages};
     cudaStream_t stream = (cudaStream_t)d->stream;
-    cudaError_t e = launch_kernel(compact_plan_kernel, kCluster, kThreads, 0, stream, 1, a);
+    const unsigned ctas = plan_ctas(d->num_pages, 0);
+    cudaError_t e = launch_kernel(compact_plan_kernel, ctas, kThreads, 0, stream, ctas, a);
     for (int i = 0; i < pool_launches(d) && e == cudaSuccess; ++i) {
         const Pools p = pools_from(d, i * kPoolsPerLaunch);
         // (half the pages at most move)

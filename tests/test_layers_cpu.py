@@ -151,6 +151,7 @@ def test_cache_refuses(lib):
     assert refusals(lib, cache(status_word=P + 1), every) == {-1}
     assert refusals(lib, cache(num_rows=1 << 20, row_pages=1 << 20), tables) == {-2}
     assert refusals(lib, cache(num_rows=262145), ("fork",)) == {-2}
+    assert refusals(lib, cache(), ("fork",), count=4097) == {-2}
     assert refusals(lib, cache(page_tokens=0), ("fork",)) == {-1}
     assert refusals(lib, cache(), ("copy", "fork", "free"), count=-1) == {-1}
     for kw in (dict(workspace=None), dict(workspace_bytes=8)):
