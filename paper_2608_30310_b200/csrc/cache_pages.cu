@@ -28,13 +28,14 @@ __device__ __forceinline__ void report(int32_t* status_word, int32_t what)
     if (status_word) *status_word = what;
 }
 
-// Item i of `pairs` x pieces: one warp moves one piece of page src[k] to page dst[k].
-__device__ void copy_pages(const Pools& pools, const int32_t* src, const int32_t* dst, uint32_t pairs, int32_t num_pages, bool check, int32_t* status_word)
+// Item i of `pairs` x pieces: one warp moves one piece of page src[k] to page dst[k].  The CTAs from `first_cta` on share the items.
+__device__ void copy_pages(const Pools& pools, const int32_t* src, const int32_t* dst, uint32_t pairs, int32_t num_pages, bool check, int32_t* status_word,
+                           uint32_t first_cta)
 {
     const uint32_t per = pools.pieces[pools.count], lane = threadIdx.x % 32;
     const uint64_t items = (uint64_t)pairs * per;
-    uint64_t i = ((uint64_t)blockIdx.x * blockDim.x + threadIdx.x) / 32;
-    const uint64_t warps = (uint64_t)gridDim.x * blockDim.x / 32;
+    uint64_t i = ((uint64_t)(blockIdx.x - first_cta) * blockDim.x + threadIdx.x) / 32;
+    const uint64_t warps = (uint64_t)(gridDim.x - first_cta) * blockDim.x / 32;
     for (; i < items; i += warps) {
         const uint32_t k = items >> 32 ? (uint32_t)(i / per) : (uint32_t)i / per, piece = (uint32_t)(i - (uint64_t)k * per);
         const int from = src[k], to = dst[k];
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(256) copy_kernel(const Pools pools, const int3
 {
     allow_successor();
     wait_for_predecessor();
-    copy_pages(pools, src, dst, pairs, num_pages, true, status_word);
+    copy_pages(pools, src, dst, pairs, num_pages, true, status_word, 0);
 }
 
 // Sum over the threads before this one, and over all of the CTA.
@@ -135,11 +136,10 @@ __device__ __forceinline__ void give_back(const ForkArgs& a, int child, int j0)
     }
 }
 
-// What a fork takes and whether it may (kCheck), the children's pages given back (kGiveBack), the free pages handed out (kTake).  Few entries: all
-// in one launch; many: the giving back is a kernel of its own between the two others, as its atomics want more SMs than a cluster has.
-constexpr int kCheck = 1, kGiveBack = 2, kTake = 4;
-
-__global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, const int steps)
+// The pages that forks take.  ALL: with the checks of the forks and the giving back before it, where there are few entries; many are given
+// back by a kernel of their own, as their atomics want more SMs than a cluster has.
+template <bool ALL>
+__global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a)
 {
     extern __shared__ int32_t forks[];               // [count] each: parent, child, pages that the child takes (the last one in part; -1: no
     __shared__ int part[32], box[kCluster];          // fork), whole pages; then the rows that are children: once or more; more than once
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, c
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, lane = tid % 32, F = a.count, W = a.row_pages;
     int32_t *parent = forks, *child = forks + F, *need = forks + 2 * F, *whole = forks + 3 * F;
     uint32_t *named = reinterpret_cast<uint32_t*>(forks + 4 * F), *twice = named + (a.num_rows + 31) / 32;
-    if (steps & kCheck)
+    if (ALL)
         for (int i = tid; i < (a.num_rows + 31) / 32; i += kThreads) named[i] = twice[i] = 0;
     cluster.sync();                                  // (all CTAs are there: they write to each other's memory)
     wait_for_predecessor();
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, c
         parent[i] = p;
         child[i] = c;
         whole[i] = n < 0 ? 0 : n / a.page_tokens;
-        if (steps & kCheck) {
+        if (ALL) {
             need[i] = n < 0 ? -1 : whole[i] + (n % a.page_tokens > 0);
             if (c < 0 || c >= a.num_rows) continue;
             const uint32_t bit = 1u << (c & 31);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, c
     }
     __syncthreads();
     const int chunks = (W + kChunk - 1) / kChunk, items = F * chunks, warps = ctas * (kThreads / 32), first = rank * (kThreads / 32) + tid / 32;
-    if (steps & kCheck) {
+    if (ALL) {
         auto has = [](const uint32_t* set, int r) { return (set[r >> 5] >> (r & 31)) & 1u; };
         for (int i = tid; i < F; i += kThreads) {
             const int p = parent[i], c = child[i];
@@ -188,12 +188,8 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, c
                 for (int r = 0; r < ctas; ++r) *(volatile int32_t*)(cluster.map_shared_rank(need, r) + i) = -1;
         }
         cluster.sync();
-        for (int i = rank * kThreads + tid; i < F; i += ctas * kThreads) {
+        for (int i = rank * kThreads + tid; i < F; i += ctas * kThreads)
             if (need[i] < 0) report(a.status_word, GDN_ERR_BAD_INDEX);
-            if (!(steps & kTake)) a.plan.need[i] = need[i];
-        }
-    }
-    if (steps & kGiveBack) {
         for (int e = first; e < items; e += warps) {
             const int i = e / chunks;
             if (need[i] >= 0) give_back(a, child[i], (e - i * chunks) * kChunk + lane);
@@ -201,7 +197,6 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, c
         cluster.sync();
     }
     allow_successor();
-    if (!(steps & kTake)) return;
     // free pages, ranked by number: each CTA counts those of its share of the pages, then lists the first `wanted`
     int wanted = 0;
     for (int i = tid; i - tid < F; i += kThreads) wanted += __syncthreads_count(i < F && need[i] > whole[i]);
@@ -241,33 +236,60 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a, c
     }
 }
 
+// The giving back of many entries, each warp for kChunk of a fork's, with the checks of the fork that fork_plan_kernel makes otherwise.
+// (No parent is a child: the rows that are checked here are not those that change.)
 __global__ void __launch_bounds__(256) give_back_kernel(const ForkArgs a)
 {
     allow_successor();
     wait_for_predecessor();
-    const int chunks = (a.row_pages + kChunk - 1) / kChunk, items = a.count * chunks;
+    const int W = a.row_pages, chunks = (W + kChunk - 1) / kChunk, items = a.count * chunks, lane = threadIdx.x % 32;
     for (int e = (blockIdx.x * blockDim.x + threadIdx.x) / 32; e < items; e += gridDim.x * blockDim.x / 32) {
-        const int i = e / chunks;
-        if (a.plan.need[i] >= 0) give_back(a, a.children[i], (e - i * chunks) * kChunk + threadIdx.x % 32);
+        const int i = e / chunks, p = a.parents[i], c = a.children[i], n = a.tokens[i];
+        const int need = n < 0 ? -1 : n / a.page_tokens + (n % a.page_tokens > 0);
+        bool ok = p >= 0 && p < a.num_rows && c >= 0 && c < a.num_rows && need >= 0 && need <= W;
+        int times = 0;
+        bool named = false;
+        for (int k = lane; k < a.count; k += 32) {
+            const int other = a.children[k];
+            times += other == c;
+            named |= other == p;
+        }
+        ok = ok && __reduce_add_sync(0xffffffffu, times) == 1 && !__any_sync(0xffffffffu, named);
+        bool bad = false;
+        for (int j0 = lane; ok && j0 < need; j0 += kChunk) {
+            int page[kChunk / 32];
+#pragma unroll
+            for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < need ? a.tables[(int64_t)p * W + j0 + 32 * u] : 0;
+#pragma unroll
+            for (int u = 0; u < kChunk / 32; ++u) bad |= page[u] < 0 || page[u] >= a.num_pages;
+        }
+        ok = ok && !__any_sync(0xffffffffu, bad);
+        if (e == i * chunks && lane == 0) {
+            a.plan.need[i] = ok ? need : -1;
+            if (!ok) report(a.status_word, GDN_ERR_BAD_INDEX);
+        }
+        if (ok) give_back(a, c, (e - i * chunks) * kChunk + lane);
     }
 }
 
-__global__ void __launch_bounds__(256) fork_kernel(const Pools pools, const ForkArgs a, const bool share)
+// The first `sharing` CTAs enter the shared pages, the others copy the partial ones.
+__global__ void __launch_bounds__(256) fork_kernel(const Pools pools, const ForkArgs a, const uint32_t sharing)
 {
     allow_successor();
     wait_for_predecessor();
-    if (share) {
+    if (blockIdx.x < sharing) {
         const int W = a.row_pages;
         const uint32_t entries = (uint32_t)a.count * W;
-        for (uint32_t e = blockIdx.x * blockDim.x + threadIdx.x; e < entries; e += gridDim.x * blockDim.x) {
+        for (uint32_t e = blockIdx.x * blockDim.x + threadIdx.x; e < entries; e += sharing * blockDim.x) {
             const int i = e / (uint32_t)W, j = e - i * W;
             if (j >= a.plan.share[i]) continue;
             const int page = a.tables[(int64_t)a.parents[i] * W + j];
             a.tables[(int64_t)a.children[i] * W + j] = page;
             atomicAdd(&a.refcounts[page], 1);
         }
+    } else {
+        copy_pages(pools, a.plan.src, a.plan.dst, a.count, a.num_pages, false, nullptr, sharing);
     }
-    copy_pages(pools, a.plan.src, a.plan.dst, a.count, a.num_pages, false, nullptr);
 }
 
 // ---- free
@@ -350,21 +372,23 @@ __global__ void __launch_bounds__(kThreads) compact_plan_kernel(const CompactArg
     }
 }
 
-__global__ void __launch_bounds__(256) compact_kernel(const Pools pools, const CompactArgs a, const bool remap)
+// The first `renaming` CTAs rewrite the tables, the others move the pages.
+__global__ void __launch_bounds__(256) compact_kernel(const Pools pools, const CompactArgs a, const uint32_t renaming)
 {
     allow_successor();
     wait_for_predecessor();
-    if (remap) {
+    if (blockIdx.x < renaming) {
         const uint32_t entries = (uint32_t)a.num_rows * a.row_pages;
-        for (uint32_t e = blockIdx.x * blockDim.x + threadIdx.x; e < entries; e += gridDim.x * blockDim.x) {
+        for (uint32_t e = blockIdx.x * blockDim.x + threadIdx.x; e < entries; e += renaming * blockDim.x) {
             const int page = a.tables[e];
             int to = -1;
             if (page >= 0 && page < a.num_pages) to = a.page_map[page];
             if (page != -1 && to < 0) report(a.status_word, GDN_ERR_BAD_INDEX);
             a.out_tables[e] = to;
         }
+    } else {
+        copy_pages(pools, a.plan.src + a.plan.header[1], a.plan.holes, a.plan.header[0], a.num_pages, false, nullptr, renaming);
     }
-    copy_pages(pools, a.plan.src + a.plan.header[1], a.plan.holes, a.plan.header[0], a.num_pages, false, nullptr);
 }
 
 // ---- host
@@ -393,7 +417,7 @@ constexpr int64_t kFewEntries = 16384;
 
 }  // namespace
 
-int fork_launches(const gdn_cache_desc* d, int32_t count) { return ((int64_t)count * d->row_pages <= kFewEntries ? 1 : 3) + pool_launches(d); }
+int fork_launches(const gdn_cache_desc* d, int32_t count) { return ((int64_t)count * d->row_pages <= kFewEntries ? 1 : 2) + pool_launches(d); }
 
 int pool_launches(const gdn_cache_desc* d) { return d->num_pools > 0 ? (d->num_pools + kPoolsPerLaunch - 1) / kPoolsPerLaunch : 1; }
 
@@ -414,22 +438,20 @@ cudaError_t launch_cache_fork(const gdn_cache_desc* d, int32_t* refcounts, int32
     ForkArgs a = {refcounts, tables, parents, children, tokens, count, d->num_pages, d->num_rows, d->row_pages, d->page_tokens, d->status_word, {}};
     int32_t* w = (int32_t*)d->workspace;
     a.plan = {w, w + count, w + 2 * (int64_t)count, w + 3 * (int64_t)count, w + 4 * (int64_t)count};
-    const size_t smem = 4 * sizeof(int32_t) * (size_t)count + 2 * sizeof(uint32_t) * ((d->num_rows + 31) / 32);
+    const int64_t entries = (int64_t)count * d->row_pages;
+    const bool all = entries <= kFewEntries;
+    const size_t smem = 4 * sizeof(int32_t) * (size_t)count + (all ? 2 * sizeof(uint32_t) * ((d->num_rows + 31) / 32) : 0);
     cudaStream_t stream = (cudaStream_t)d->stream;
     cudaError_t e = cudaSuccess;
-    if (smem > 40 * 1024) e = cudaFuncSetAttribute(fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    const int64_t entries = (int64_t)count * d->row_pages;
-    const unsigned ctas = plan_ctas(d->num_pages, entries);
-    if (e == cudaSuccess && entries <= kFewEntries) {
-        e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a, kCheck | kGiveBack | kTake);
-    } else if (e == cudaSuccess) {
-        e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a, kCheck);
-        if (e == cudaSuccess) e = launch_kernel(give_back_kernel, grid_for(0, entries), 256, 0, stream, 1, a);
-        if (e == cudaSuccess) e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a, kTake);
-    }
+    auto plan = all ? fork_plan_kernel<true> : fork_plan_kernel<false>;
+    if (smem > 40 * 1024) e = cudaFuncSetAttribute(plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const unsigned ctas = plan_ctas(d->num_pages, all ? entries : 0);
+    if (e == cudaSuccess && !all) e = launch_kernel(give_back_kernel, grid_for(0, entries), 256, 0, stream, 1, a);
+    if (e == cudaSuccess) e = launch_kernel(plan, ctas, kThreads, smem, stream, ctas, a);
     for (int i = 0; i < pool_launches(d) && e == cudaSuccess; ++i) {
         const Pools p = pools_from(d, i * kPoolsPerLaunch);
-        e = launch_kernel(fork_kernel, grid_for((uint64_t)count * p.pieces[p.count], (uint64_t)count * d->row_pages), 256, 0, stream, 1, p, a, i == 0);
+        const unsigned sharing = i == 0 ? grid_for(0, entries) : 0;
+        e = launch_kernel(fork_kernel, sharing + grid_for((uint64_t)count * p.pieces[p.count], 0), 256, 0, stream, 1, p, a, sharing);
     }
     return e;
 }
@@ -451,8 +473,9 @@ cudaError_t launch_cache_compact(const gdn_cache_desc* d, const int32_t* refcoun
     cudaError_t e = launch_kernel(compact_plan_kernel, ctas, kThreads, 0, stream, ctas, a);
     for (int i = 0; i < pool_launches(d) && e == cudaSuccess; ++i) {
         const Pools p = pools_from(d, i * kPoolsPerLaunch);
+        const unsigned renaming = i == 0 ? grid_for(0, (uint64_t)d->num_rows * d->row_pages) : 0;
         // (half the pages at most move)
-        e = launch_kernel(compact_kernel, grid_for((uint64_t)d->num_pages / 2 * p.pieces[p.count], (uint64_t)d->num_rows * d->row_pages), 256, 0, stream, 1, p, a, i == 0);
+        e = launch_kernel(compact_kernel, renaming + grid_for((uint64_t)d->num_pages / 2 * p.pieces[p.count], 0), 256, 0, stream, 1, p, a, renaming);
     }
     return e;
 }
