@@ -215,7 +215,7 @@ GDN_API int64_t tail_select(int64_t prefix_len, double budget_frac);
 /*
  * ---- Recurrent layers beside the Gated DeltaNet: short convolution and selective scan ----
  *
- * What stands before and beside the recurrence above in hybrid models.  Device pointers only.  Prompts are packed as above
+ * What stands before and beside the recurrence above in hybrid models.  Device pointers only, of the current device.  Prompts are packed as above
  * (cu_tail_lens: request n owns rows [cu[n], cu[n+1])); total_tokens may exceed cu[num_seqs] (a padded batch): rows from
  * cu[num_seqs] on are neither read nor written.  Row strides are in elements, between consecutive tokens; the last dimension is
  * packed.  Any alignment is served; the vector path needs 16-byte aligned rows.  The states lie in pools:

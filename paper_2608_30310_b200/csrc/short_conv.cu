@@ -4,8 +4,8 @@
 //
 // A thread has VEC neighbouring channels and walks R rows of the packed batch with the last K - 1 rows in registers, so that every
 // row is read once, but for the K - 1 rows before a thread's first.  Where a request begins inside the walk, the window is refilled
-// from the request's start state, and the same thread writes the request's final state: it has read the start state by then, so that
-// both may be the same memory.  Bound by HBM: 2 K + 4 flops and two special-function results a value against 4 bytes moved (bf16).
+// from the request's start state, and the same thread writes the request's final state; it also goes on for the K - 1 rows that need the
+// start state, past the end of its share if need be.  So no other thread reads the start state, and both may be the same memory.  Bound by HBM: 2 K + 4 flops and two special-function results a value against 4 bytes moved (bf16).
 #include "layers.cuh"
 
 namespace gdn {
@@ -50,11 +50,6 @@ struct Window {
         }
         if (a.bias) bias = widened<T, VEC>(*reinterpret_cast<const Pack<T, VEC>*>(static_cast<const T*>(a.bias) + c));
         else bias = {};
-    }
-    __device__ __forceinline__ void clear()
-    {
-#pragma unroll
-        for (int j = 0; j < K - 1; ++j) hist[j] = {};
     }
     __device__ __forceinline__ void set(int j, const Pack<T, VEC>& p) { hist[j] = widened<T, VEC>(p); }
     // the next row in, its result out
@@ -140,16 +135,13 @@ __global__ void __launch_bounds__(128, kResident) short_conv_kernel(const ConvAr
         const int mid = (n + hi) / 2;
         if (a.cu[mid] < t0) n = mid + 1; else hi = mid;
     }
-    if (n > 0 && t0 < min(a.cu[n], t1)) {                    // (cu[n] > t0: otherwise it begins here)
-        const int begin = a.cu[n - 1], slot = init && t0 - begin < K - 1 ? slot_of(a.init_slots, n - 1, a.num_init, a.status_word) : -1;
-        win.clear();
+    if (n > 0) {                                             // a request that began before: its first K - 1 rows are not this walk's
+        const int begin = a.cu[n - 1], from = max(t0, begin + K - 1), end = min(a.cu[n], t1);
+        if (from < end) {
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j) {
-            const int t = t0 - (K - 1) + j;
-            if (t >= begin) win.set(j, row(t));
-            else if (slot >= 0) win.set(j, *reinterpret_cast<const P*>(init + ((int64_t)slot * (K - 1) + (K - 1 + t - begin)) * a.channels));
+            for (int j = 0; j < K - 1; ++j) win.set(j, row(from - (K - 1) + j));
+            walk(from, end);
         }
-        walk(t0, min(a.cu[n], t1));
     }
     for (; n < N; ++n) {
         const int begin = a.cu[n], end = min(a.cu[n + 1], last);
@@ -180,7 +172,7 @@ __global__ void __launch_bounds__(128, kResident) short_conv_kernel(const ConvAr
                 *reinterpret_cast<P*>(s + (int64_t)j * a.channels) = p;
             }
         }
-        walk(begin, min(end, t1));
+        walk(begin, min(end, max(t1, begin + K - 1)));       // (as many rows as need the start state)
     }
 }
 

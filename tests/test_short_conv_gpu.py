@@ -178,6 +178,29 @@ def test_slots():
     assert int(status) == -7
 
 
+@pytest.mark.parametrize("dtype,C", [(BF, 8), (F32, 3), (BF, 512)])
+@pytest.mark.parametrize("K", [2, 3, 4])
+def test_states_in_place_wherever_requests_begin(dtype, C, K):
+    """Requests of all short lengths, one behind the other, so that they begin at every place of a thread's share of rows: the thread that
+    replaces a start state is the only one that reads it."""
+    rng = np.random.default_rng(K)
+    lens = [int(v) for v in rng.permutation(np.repeat(np.arange(0, 21), 30))] + [40]
+    x, w, b = inputs(sum(lens), C, K, dtype, 70)
+    N = len(lens)
+    init = torch.randn((N, K - 1, C), generator=torch.Generator().manual_seed(6)).to(dtype)
+    cols = list(range(C))[:5]
+    ref, bound, rs = conv_ref(x[:, cols], w[cols], b[cols], lens, init[:, :, cols])
+    xd, wd, bd, cu = x.cuda(), w.cuda(), b.cuda(), cu_of(lens).cuda()
+    first = None
+    for _ in range(5):
+        pool, out = init.cuda(), torch.empty_like(xd)
+        gdn().gdn_short_conv(xd, wd, bd, cu, out, init_state=pool, out_state=pool)
+        within(out.cpu()[:, cols], ref, bound)
+        assert torch.equal(pool[:, :, cols].cpu(), rs)
+        assert first is None or torch.equal(out, first)
+        first = out
+
+
 def test_a_request_alone_in_a_longer_batch_array():
     """No rows at all, no requests, only empty requests."""
     w, b = (t.cuda() for t in inputs(0, 8, 4, F32, 1)[1:])
