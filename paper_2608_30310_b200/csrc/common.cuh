@@ -49,13 +49,15 @@ struct Sched {
 // Kernel launch that may begin while the kernel before it in the stream is still running (programmatic dependent launch): the
 // launch itself and a kernel's start-up pass under the tail of its predecessor.  Every kernel so launched calls
 // wait_for_predecessor() before its first access to global memory, and allow_successor() as early as it likes.
-template <typename... P, typename... A>
+// EARLY = false: the kernel begins when its predecessor has ended, as an ordinary launch does.  For kernels whose CTAs fill the GPU only when
+// they are spread evenly: begun early they crowd the SMs that their predecessor has left by then.
+template <bool EARLY = true, typename... P, typename... A>
 inline cudaError_t launch_kernel(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster, A&&... args)
 {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[0].val.programmaticStreamSerializationAllowed = EARLY;
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;

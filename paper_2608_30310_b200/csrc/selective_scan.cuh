@@ -383,7 +383,7 @@ template <typename T, typename F> cudaError_t launch_form(const ScanArgs& a, cud
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    return launch_kernel(kernel, (unsigned)grid, kThreads, smem, stream, 1, a, tiles);
+    return launch_kernel<false>(kernel, (unsigned)grid, kThreads, smem, stream, 1, a, tiles);
 }
 
 // How many states a lane holds.  With fewer there are more warps, and each is sooner done with a row; with more, what is done once per lane

@@ -80,7 +80,6 @@ __global__ void __launch_bounds__(128, kResident) short_conv_kernel(const ConvAr
 {
     using P = Pack<T, VEC>;
     const uint32_t id = blockIdx.x * 128u + threadIdx.x, tile = id / vectors, c = (id - tile * vectors) * VEC;
-    allow_successor();
     wait_for_predecessor();
     if (tile >= tiles) return;
     const int N = a.num_seqs, last = (int)min((int64_t)a.cu[N], a.total_tokens);
@@ -174,6 +173,7 @@ __global__ void __launch_bounds__(128, kResident) short_conv_kernel(const ConvAr
         }
         walk(begin, min(end, max(t1, begin + K - 1)));       // (as many rows as need the start state)
     }
+    allow_successor();                                       // (at the end: an early successor would be spread over the SMs that are free by then)
 }
 
 // One token per request: the window is the request's state.
