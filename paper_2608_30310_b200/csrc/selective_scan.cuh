@@ -49,10 +49,12 @@ template <int S_, int SS_, int CC_, typename T> struct Form {
     static constexpr int SUMS = TS * CC, MINE = SUMS / LN;   // sums of a reduction, and how many a lane ends up with
     static constexpr int PER = TB * CT / (32 * kHelpers);    // channels of a row that a helper has in hand at once
     static constexpr int VE = PER > 8 ? 8 : PER < 2 ? 2 : PER, ROWI = CT / VE, ITEMS = TB * ROWI, IPT = (ITEMS + 32 * kHelpers - 1) / (32 * kHelpers);
-    // (dt, dt x) of two channels are 16 bytes; those of an item's channels 0 and 1, of all items of the row, come first, then those of channels
-    // 2 and 3, and so on, and y likewise by 16 or 8 bytes: so that neighbouring lanes access neighbouring 16 bytes.
-    static constexpr int PS = 2 * CT + (2 * CT % 32 == 0 && ROWI < 8 ? 16 : 0), YV = VE < 4 ? VE : 4, YS = CT + 8;
-    __host__ __device__ static constexpr int p_at(int ch) { return (ch % VE / 2 * ROWI + ch / VE) * 4 + ch % 2 * 2; }
+    // (dt, dt x) of two channels are 16 bytes; those of an item's channels 0 and 1, of all items of the row, come first (neighbouring lanes write
+    // neighbouring 16 bytes), then, four words further on (a compute warp's channels are in different banks), those of channels 2 and 3, and
+    // so on; y likewise by 16 or 8 bytes.
+    static constexpr int PJ = 4 * ROWI + 4, PW = VE / 2 * PJ, PS = ROWI >= 8 ? PW : PW + (4 * ROWI - PW % 32 + 32) % 32;
+    static constexpr int YV = VE < 4 ? VE : 4, YS = CT + 4;
+    __host__ __device__ static constexpr int p_at(int ch) { return ch % VE / 2 * PJ + ch / VE * 4 + ch % 2 * 2; }
     __host__ __device__ static constexpr int y_at(int ch) { return (ch % VE / YV * ROWI + ch / VE) * YV + ch % YV; }
     static_assert(TB % TS == 0 && SUMS % LN == 0 && W * LN == 32 * CC && CT % VE == 0, "");
     static constexpr int BC = sizeof(T) == 2 ? 1 : 2;        // words of (b, c): packed bf16 halves, or one each
@@ -68,7 +70,7 @@ template <int S_, int SS_, int CC_, typename T> struct Form {
 
 // ALIGNED: rows of x, dt, z and out, and the channels of a group, come in whole vectors of VE values, rows of b and c in whole 8 bytes.
 template <typename T, typename F, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, 3) selective_scan_kernel(const ScanArgs a, const uint32_t tiles)
+__global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective_scan_kernel(const ScanArgs a, const uint32_t tiles)
 {
     constexpr int S = F::S, SS = F::SS, CC = F::CC, LN = F::LN, W = F::W, CT = F::CT, VE = F::VE, TB = F::TB, TS = F::TS;
     extern __shared__ __align__(16) unsigned char raw[];
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 3) selective_scan_kernel(const ScanA
                     const float2 dv = parts(d), dx = parts(mul(d, pair_at(x, v)));
                     float4 q = make_float4(dv.x, dx.x, dv.y, dx.y);
                     if (r >= left) q = make_float4(0.f, 0.f, 0.f, 0.f);
-                    *reinterpret_cast<float4*>(&sh.p[buf][r * F::PS + F::p_at(ch) + v / 2 * F::ROWI * 4]) = q;
+                    *reinterpret_cast<float4*>(&sh.p[buf][r * F::PS + F::p_at(ch) + v / 2 * F::PJ]) = q;
                 }
             }
 #pragma unroll
