@@ -52,7 +52,7 @@ struct Sched {
 // EARLY = false: the kernel begins when its predecessor has ended, as an ordinary launch does.  For kernels whose CTAs fill the GPU only when
 // they are spread evenly: begun early they crowd the SMs that their predecessor has left by then.
 template <bool EARLY = true, typename... P, typename... A>
-inline cudaError_t launch_kernel(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster, A&&... args)
+inline cudaError_t launch_kernel(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster, A&&... args)
 {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];

@@ -30,7 +30,19 @@ __device__ __forceinline__ F2 softplus_of(F2 x2)
     p = fma(u, p, both(0.9999999694f));
     return fma(u, p, pair(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
 }
-__device__ __forceinline__ float softplus_of(float x) { return parts(softplus_of(both(x))).x; }
+__device__ __forceinline__ float softplus_of(float x)
+{
+    const float u = ex2(-kLog2e * fabsf(x));
+    float p = fmaf(u, 0.005232692641f, -0.02950523219f);
+    p = fmaf(u, p, 0.07822594086f);
+    p = fmaf(u, p, -0.136632448f);
+    p = fmaf(u, p, 0.191060062f);
+    p = fmaf(u, p, -0.2484298196f);
+    p = fmaf(u, p, 0.3331909665f);
+    p = fmaf(u, p, -0.4999949302f);
+    p = fmaf(u, p, 0.9999999694f);
+    return fmaf(u, p, fmaxf(x, 0.f));
+}
 
 template <typename T, int N> __device__ __forceinline__ void load_values(const T* p, float (&v)[N])
 {
