@@ -275,6 +275,21 @@ def test_captured():
         c.agrees()
 
 
+@pytest.mark.parametrize("children,row", [(40, 30), (40, 600)])
+def test_forks_left_out_among_many(children, row):
+    """The same rules where the rows are long, and a kernel of its own gives them back, as where they are short."""
+    rng = random.Random(row)
+    c = Cache(children * row // 2, children + 8, row, (64,))
+    c.fill([row, row // 2, row] + [0] * 5 + [rng.randint(0, row // 8) for _ in range(children)], rng)
+    c.table[2][row // 3] = len(c.count) + 5                                 # a broken parent
+    c.upload()
+    who = [rng.randrange(3) for _ in range(children)]
+    kids = list(range(8, 8 + children))
+    tokens = [rng.randint(0, row * 16) for _ in range(children)]
+    kids[5], kids[6], who[7], who[9], tokens[11], kids[13] = kids[4], 8 + children + 3, kids[1], -1, row * 16 + 1, -7
+    c.fork(who, kids, tokens, status=-7)
+
+
 def test_refused_tensors():
     c = Cache(16, 3, 4)
     c.upload()

@@ -59,7 +59,7 @@ LENS = [[1], [0, 3, 0], [31, 32, 33, 0, 65, 1], [130, 7]]
 def test_prompts(dtype, S, C, G, lens):
     m = scan_inputs(sum(lens), C, S, G, dtype, seed=S + C)
     init = torch.randn((len(lens), C, S), generator=torch.Generator().manual_seed(9)) if C != 24 else None
-    check(m, lens, init, gate=C != 72, skip=C != 7, bias=C != 64, pad=4 if C == 1 else 0)
+    check(m, lens, init, gate=C != 72, skip=C != 7, bias=C != 64, pad=4 if C in (1, 64) else 0)
 
 
 # From few states in a call to many: every form of the kernel for each number of states, with channels that fill its tiles and that do not.
@@ -224,6 +224,37 @@ def test_slots():
     gdn().gdn_selective_scan_step(d["x"][:2], d["dt"][:2], d["a"], d["b"][:2], d["c"][:2], dev, out[:2], dev,
                                   slots=torch.tensor([1, 6], dtype=torch.int32, device="cuda"), status_word=status)
     assert int(status) == -7
+
+
+def test_two_streams_and_a_thread_each():
+    """Calls at once, from two threads on two streams, share nothing."""
+    import threading
+    jobs = []
+    for i in range(2):
+        lens = [300 + 100 * i, 50, 7]
+        m = scan_inputs(sum(lens), 256, 16, 1, BF, 80 + i)
+        ref, st = run(m, lens)
+        jobs.append((lens, {k: v.cuda() for k, v in m.items()}, ref, st, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    outs = [[], []]
+
+    def work(i):
+        lens, d, _, _, stream = jobs[i]
+        cu = cu_of(lens).cuda()
+        torch.cuda.synchronize()
+        for _ in range(40):
+            o, p = torch.empty_like(d["x"]), torch.empty(3, 256, 16, device="cuda")
+            torch.cuda.current_stream().synchronize()
+            gdn().gdn_selective_scan(d["x"], d["dt"], d["a"], d["b"], d["c"], cu, o, d=d["d"], z=d["z"], dt_bias=d["dt_bias"], out_state=p, stream=stream)
+            outs[i].append((o, p))
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(outs[i]) == 40
+        for o, p in outs[i]:
+            assert torch.equal(o, jobs[i][2]) and torch.equal(p, jobs[i][3])
 
 
 def test_no_rows():

@@ -56,7 +56,7 @@ LENS = [[1], [2, 1, 3], [0, 5, 0, 0, 64, 1, 0], [7, 8, 9, 63, 130, 0], [300]]
 def test_prompts(dtype, K, C, lens):
     x, w, b = inputs(sum(lens), C, K, dtype, seed=C + K)
     init = torch.randn((len(lens), K - 1, C), generator=torch.Generator().manual_seed(9)).to(dtype) if C != 8 else None
-    out, states = run(x, w, b if C != 36 else None, lens, init, act=C != 136, pad=5 if C == 1 else 0)
+    out, states = run(x, w, b if C != 36 else None, lens, init, act=C != 136, pad=5 if C in (1, 136) else 0)
     ref, bound, rs = conv_ref(x, w, b if C != 36 else None, lens, init, act=C != 136)
     within(out, ref, bound, "out")
     assert torch.equal(states, rs)
