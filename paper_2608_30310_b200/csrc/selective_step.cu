@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(128) selective_step_kernel(const ScanArgs a)
         for (int q = 0; q < Q; ++q) {
 #pragma unroll
             for (int s = 0; s < 4; s += 2) {
-                const float2 e = parts(mul(arg, pair_at(d[k][q], s)));
+                const float2 e = parts(fma(arg, pair_at(d[k][q], s), both(kLift)));
                 const F2 hn = fma(pair(ex2(e.x), ex2(e.y)), pair_at(h[k][q], s), mul(dx, pair_at(b[GROUPS ? k : 0][q], s)));
                 acc = fma(hn, pair_at(c[GROUPS ? k : 0][q], s), acc);
                 const float2 v = parts(hn);
