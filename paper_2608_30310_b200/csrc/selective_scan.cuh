@@ -10,7 +10,7 @@
 // barrier per block.
 //
 // Bound by its exponentials, not by memory: one result of the special-function unit per state and token, three more per channel and token.
-// Eight hits (12,616 tokens, 4,096 channels, 16 states, bf16) take 302 us where the unit alone would take 219 and the memory 65; issue
+// Eight hits (12,616 tokens, 4,096 channels, 16 states, bf16) take 302 us where the unit alone would take 215 and the memory 65; issue
 // slots, unit and shared memory are 68-73 % busy.  One request of 1,638 tokens: 62 us (unit 28), one compute and one helper warp per
 // scheduler, latency.  Everything in every warp, without roles, took 1,050 and 174 us.  32 rows a block: sixteen 334 us for eight hits.
 #pragma once
