@@ -75,10 +75,11 @@ def test_every_form(dtype, S, values, C, G):
     check(m, lens, torch.randn((N, C, S), generator=torch.Generator().manual_seed(2)))
 
 
-@pytest.mark.parametrize("N", [63, 64, 65, 300])
-def test_many_requests(N):
-    """Up to 64 requests are taken longest first, more in the order given."""
-    lens = [int(v) for v in np.random.default_rng(N).integers(0, 12, size=N)]
+@pytest.mark.parametrize("N,most", [(63, 12), (64, 12), (65, 12), (300, 12), (2, 500), (33, 350), (64, 320)])
+def test_many_requests(N, most):
+    """Up to 64 requests of 128 tokens and more in the mean are taken longest first, others in the order given."""
+    lens = [int(v) for v in np.random.default_rng(N).integers(0, most, size=N)]
+    lens[-1] = most
     check(scan_inputs(sum(lens), 40, 16, 1, BF, N), lens, torch.randn((N, 40, 16), generator=torch.Generator().manual_seed(2)))
 
 
