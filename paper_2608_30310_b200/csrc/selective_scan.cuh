@@ -402,6 +402,7 @@ template <typename T, typename F> cudaError_t launch_form(const ScanArgs& a, cud
     const uintptr_t bc = (uintptr_t)a.b | (uintptr_t)a.c | (uintptr_t)((a.b_stride | a.c_stride) * (int64_t)sizeof(T));
     const bool aligned = all % alignof(Pack<T, F::VE>) == 0 && bc % 8 == 0 && each % F::VE == 0;
     constexpr size_t smem = sizeof(typename F::Shared);
+    static_assert(smem <= 227 * 1024, "what a CTA can have");
     // Longest first, up to the number of requests that a CTA orders itself, unless they are short: 64 of 64 tokens 140 us ordered, 121 not;
     // 16 of 33-700 tokens 181, 189; eight of 410-3,277 303, 429.
     const bool ordered = a.num_seqs > 1 && a.num_seqs <= kSelfSort && a.total_tokens >= 128ll * a.num_seqs;
@@ -417,14 +418,16 @@ template <typename T, typename F> cudaError_t launch_form(const ScanArgs& a, cud
 // and row (loads, sums) serves more of them.  By the states of the call per SM (requests x channels x states / 148); measured at 16
 // states, bf16, us with one / two / four states a lane: one request of 1,638 tokens and 1,024 channels (111 per SM) 30 / 40 / 59; 2,048 channels
 // (221) 49 / 40 / 59; 4,096 channels (443) 92 / 64 / 60; eight hits of 4,096 channels (3,542) 582 / 379 / 303.  fp32 reads twice the
-// words of b and c per state: there four states are two of two channels each, which share them (eight hits 417 -> 375), from more states on
-// (4,096 channels 71 with two a lane, 83).  64 states are summed over 16 lanes: two channels a lane halve that (4,096 channels 205 -> 168).
+// words of b and c per state, which two channels a lane share: four states of two channels, from more states on (4,096 channels 71 with
+// two states a lane, 72 so; eight hits 445, 366; four states of one channel 398, two of two 375).  64 states are summed over 16 lanes, which two
+// channels a lane halve (bf16, 4,096 channels 205 -> 168).  With 8 states that form's tiles do not fit the shared memory in fp32: two by two.
 template <typename T, int S> cudaError_t launch_states(const ScanArgs& a, cudaStream_t stream)
 {
     const int64_t per_sm = (int64_t)a.num_seqs * a.channels * S / 148;
     if (S < 64 && per_sm <= 160) return launch_form<T, Form<S, S < 64 ? 1 : 2, 1, T>>(a, stream);
     if (per_sm <= (sizeof(T) == 2 ? 320 : 700)) return launch_form<T, Form<S, 2, 1, T>>(a, stream);
-    return launch_form<T, Form<S, sizeof(T) == 2 ? 4 : 2, sizeof(T) == 2 && S < 64 ? 1 : 2, T>>(a, stream);
+    constexpr bool half = sizeof(T) == 2;
+    return launch_form<T, Form<S, !half && S == 8 ? 2 : 4, half && S < 64 ? 1 : 2, T>>(a, stream);
 }
 
 template <typename T> cudaError_t launch_type(const ScanArgs& a, int states, cudaStream_t stream)
