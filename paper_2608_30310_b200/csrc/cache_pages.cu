@@ -15,7 +15,7 @@ namespace cg = cooperative_groups;
 namespace gdn {
 namespace {
 
-constexpr int kCluster = 8, kThreads = 1024, kChunk = 256;
+constexpr int kCluster = 8, kThreads = 512, kChunk = 256;
 constexpr int64_t kPiece = 4096;       // bytes that a warp moves at a time
 constexpr int kPoolsPerLaunch = 64;
 
@@ -83,7 +83,7 @@ __device__ int scan_cta(int v, int* total, int* part)
     }
     if (lane == 31) part[warp] = x;
     __syncthreads();
-    int w = part[lane];
+    const int w = lane < kThreads / 32 ? part[lane] : 0;
     const int before_warp = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
     *total = __reduce_add_sync(0xffffffffu, w);
     __syncthreads();
@@ -145,7 +145,7 @@ template <bool ALL>
 __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a)
 {
     extern __shared__ int32_t forks[];               // [count] each: parent, child, pages that the child takes (the last one in part; -1: no
-    __shared__ int part[32], box[kCluster];          // fork), whole pages; then the rows that are children: once or more; more than once
+    __shared__ int part[kThreads / 32], box[kCluster];          // fork), whole pages; then the rows that are children: once or more; more than once
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, lane = tid % 32, F = a.count, W = a.row_pages;
     int32_t *parent = forks, *child = forks + F, *need = forks + 2 * F, *whole = forks + 3 * F;
@@ -336,7 +336,7 @@ struct CompactArgs {
 
 __global__ void __launch_bounds__(kThreads) compact_plan_kernel(const CompactArgs a)
 {
-    __shared__ int part[32], box[kCluster];
+    __shared__ int part[kThreads / 32], box[kCluster];
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), tid = threadIdx.x, P = a.num_pages;
     cluster.sync();                                  // (all CTAs are there: they write to each other's memory)
