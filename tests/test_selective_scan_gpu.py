@@ -93,6 +93,20 @@ def test_without_softplus_and_with_extreme_time_steps():
     check(m, [50, 40], torch.randn((2, 32, 16), generator=torch.Generator().manual_seed(2)), bias=False)
 
 
+def test_a_group_for_every_channel_and_rows_before_the_first_request():
+    """As many groups as channels; and cu_tail_lens that begins above zero, as a slice of a longer batch's does: other rows stay."""
+    lens = [20, 45]
+    m = scan_inputs(65, 9, 8, 9, F32, 8)
+    check(m, lens)
+    ref, bound, _, _ = scan_ref(m["x"], m["dt"], m["a"], m["b"], m["c"], lens, m["d"], m["z"], m["dt_bias"])
+    d = {k: v.cuda() for k, v in m.items()}
+    out = torch.full_like(d["x"], 6.0)
+    gdn().gdn_selective_scan(d["x"], d["dt"], d["a"], d["b"], d["c"], torch.tensor([20, 65], dtype=torch.int32, device="cuda"), out, d=d["d"], z=d["z"],
+                             dt_bias=d["dt_bias"])
+    assert bool((out[:20] == 6).all())
+    within(out[20:], ref[20:], bound[20:])
+
+
 def test_slow_decay_over_a_long_request():
     """Time steps of 0.001 over 6,000 tokens: the states hold sums over a thousand tokens."""
     m = scan_inputs(6000, 4, 16, 1, F32, 7)

@@ -104,6 +104,18 @@ def test_other_requests_values_do_not_matter():
                 assert torch.equal(out[cu[m]:cu[m + 1]].view(torch.int16), clean[cu[m]:cu[m + 1]].view(torch.int16)) and torch.equal(s1[m], s0[m])
 
 
+def test_rows_before_the_first_request():
+    """cu_tail_lens that begins above zero, as a slice of a longer batch's does: other rows are neither read nor written."""
+    x, w, b = inputs(200, 16, 4, F32, 13)
+    y = x.clone()
+    y[:77] = float("nan")
+    out = torch.full((200, 16), 6.0, device="cuda")
+    gdn().gdn_short_conv(y.cuda(), w.cuda(), b.cuda(), torch.tensor([77, 90, 190], dtype=torch.int32, device="cuda"), out)
+    ref, bound, _ = conv_ref(x[77:190], w, b, [13, 100])
+    assert bool((out[:77] == 6).all()) and bool((out[190:] == 6).all())
+    within(out[77:190], ref, bound)
+
+
 def test_values_at_the_ends_of_the_range():
     """Large negative results vanish, infinities and NaN stay where the formula has them."""
     x = torch.tensor([[1e4], [-1e4], [float("inf")], [0.0], [0.0], [0.0], [-200.0], [float("nan")], [1.0]])
