@@ -37,16 +37,18 @@ struct Window {
     {
         silu = a.silu;
         const T* weight = static_cast<const T*>(a.weight) + (size_t)c * K;
-        Pack<T, VEC * K> p;
-        if (VEC > 1) p = *reinterpret_cast<const Pack<T, VEC * K>*>(weight);
-        else
+        T p[VEC * K];                                        // (of channel 0, then of channel 1, ...)
 #pragma unroll
-            for (int j = 0; j < K; ++j) p.v[j] = weight[j];
+        for (int j = 0; j < K; ++j) {                        // in packs as wide as the rows': the alignment that the choice of VEC asks of the weights
+            const Pack<T, VEC> q = *reinterpret_cast<const Pack<T, VEC>*>(weight + j * VEC);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) p[j * VEC + v] = q.v[v];
+        }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             Pack<T, VEC> q;
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) q.v[v] = p.v[v * K + j];
+            for (int v = 0; v < VEC; ++v) q.v[v] = p[v * K + j];
             w[j] = widened<T, VEC>(q);
         }
         if (a.bias) bias = widened<T, VEC>(*reinterpret_cast<const Pack<T, VEC>*>(static_cast<const T*>(a.bias) + c));
@@ -227,6 +229,7 @@ template <typename T>
 cudaError_t launch_width(const ConvArgs& a, int width, bool step, cudaStream_t stream)
 {
     constexpr int VEC = 4;
+    static_assert(alignof(Pack<T, VEC>) == VEC * sizeof(T), "what the kernels load at once is what is checked here");
     const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.weight | (uintptr_t)a.bias | (uintptr_t)a.init_state | (uintptr_t)a.out |
                           (uintptr_t)a.out_state | (uintptr_t)((a.x_stride | a.out_stride) * (int64_t)sizeof(T));
     const bool vec = (all & (VEC * sizeof(T) - 1)) == 0 && a.channels % VEC == 0;
