@@ -334,8 +334,10 @@ GDN_API int32_t gdn_cache_copy(const gdn_cache_desc* desc, const int32_t* src, c
  * Row children[i] becomes a branch of row parents[i] after tokens[i] tokens, for i < count: the pages that the child held are given
  * back; the tokens / page_tokens whole pages are shared (their counts go up); where tokens end inside a page, that page is copied to a
  * free one, which the child alone holds; the rest of the child's row is -1.  All children give back before any takes a page.
- * A child may be named once and may not be a parent in the same call; tokens fit the row; the parent holds pages for them.  A fork that
- * breaks this is left out, its child's row as it was (GDN_ERR_BAD_INDEX).  Too few free pages: the forks that get none, the last ones
+ * A child may be named once and may not be a parent in the same call; tokens fit the row; the parent holds pages for them, each with a
+ * count above 0.  A fork that breaks this is left out, its child's row as it was (GDN_ERR_BAD_INDEX).  (A page's count is at least the number
+ * of entries that name it, as the calls leave it; whether a smaller one that is not 0 serves is not defined.)  A child's entries are given
+ * back as by gdn_cache_free.  Too few free pages: the forks that get none, the last ones
  * that need one, leave their child's row empty (GDN_ERR_NO_PAGES).  At most GDN_CACHE_MAX_ROWS rows and GDN_CACHE_MAX_FORKS forks.
  */
 #define GDN_CACHE_MAX_ROWS 262144

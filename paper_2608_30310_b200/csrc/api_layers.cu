@@ -175,7 +175,7 @@ int32_t gdn_cache_fork(const gdn_cache_desc* d, int32_t* refcounts, int32_t* tab
     if (count == 0) return GDN_OK;
     if (!ints(refcounts) || !ints(tables) || !ints(parents) || !ints(children) || !ints(tokens)) return GDN_ERR_INVALID_ARG;
     if ((rc = check_workspace(d, count)) != GDN_OK) return rc;
-    return done(gdn::launch_cache_fork(d, refcounts, tables, parents, children, tokens, count), gdn::fork_launches(d, count));
+    return done(gdn::launch_cache_fork(d, refcounts, tables, parents, children, tokens, count), gdn::fork_launches(d));
 }
 
 int32_t gdn_cache_free(const gdn_cache_desc* d, int32_t* refcounts, int32_t* tables, const int32_t* rows, int32_t count)

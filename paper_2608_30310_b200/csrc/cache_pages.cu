@@ -5,8 +5,9 @@
 // per warp, eight 16-byte loads in flight per lane; it is bound by HBM.  Nothing depends on the order in which threads run: free pages
 // are ranked by number, counts change by atomic integer additions.
 //
-// 400 pages of 12 pools, 64 KB each: 102 us, 6.1 TB/s, 95 % of the measured copy rate; 512 of 2,048 pages moved by a compaction 136 us (92 %, planning
-// included).  64 forks of prefixes of 2,048 pages: 20 us for 24 MB, three dependent kernels.
+// 400 pages of 12 pools, 64 KB each: 102 us, 6.1 TB/s, 95 % of the measured copy rate; 512 of 2,048 pages moved by a compaction 135 us (92 %, planning
+// included).  64 forks of prefixes of 2,048 pages: 18 us for 24 MB, three dependent kernels.  A fork reads its parent's row once, and the count
+// of each page there: 64 rows of 32,768 entries 81 us.
 #include <cooperative_groups.h>
 #include "cache_pages.cuh"
 
@@ -15,7 +16,7 @@ namespace cg = cooperative_groups;
 namespace gdn {
 namespace {
 
-constexpr int kCluster = 8, kThreads = 512, kChunk = 256;
+constexpr int kCluster = 8, kThreads = 512;
 constexpr int64_t kPiece = 4096;       // bytes that a warp moves at a time
 constexpr int kPoolsPerLaunch = 64;
 
@@ -119,90 +120,109 @@ struct ForkArgs {
     ForkPlan plan;
 };
 
-// kChunk entries of the child's row of fork i, from its entry j0 on (lanes 32 apart), given back
-__device__ __forceinline__ void give_back(const ForkArgs& a, int child, int j0)
+// Entries of a row in a thread's hands, all of them on their way at once: kHand, `step` apart from entry j0 on.
+constexpr int kHand = 8;
+__device__ __forceinline__ void entries_of(const int32_t* row, int64_t j0, int step, int end, int beyond, int (&page)[kHand])
 {
-    int32_t* row = a.tables + (int64_t)child * a.row_pages;
-    int page[kChunk / 32], held[kChunk / 32];
 #pragma unroll
-    for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < a.row_pages ? row[j0 + 32 * u] : -1;
+    for (int u = 0; u < kHand; ++u) page[u] = j0 + u * step < end ? row[j0 + u * step] : beyond;
+}
+
+// Whether entries of a parent's row before `end` name pages that are held.  A page that the row holds in earnest keeps its count above 0 whoever
+// gives back meanwhile; one that is free could be handed to another fork.
+__device__ __forceinline__ bool all_held(const ForkArgs& a, const int32_t* row, int64_t j0, int step, int end)
+{
+    int page[kHand], count[kHand];
+    bool ok = true;
+    entries_of(row, j0, step, end, 0, page);
 #pragma unroll
-    for (int u = 0; u < kChunk / 32; ++u) {
-        if (page[u] != -1) row[j0 + 32 * u] = -1;
+    for (int u = 0; u < kHand; ++u) {
+        const bool real = page[u] >= 0 && page[u] < a.num_pages;
+        count[u] = j0 + u * step < end ? (real ? __ldcg(&a.refcounts[page[u]]) : 0) : 1;
+    }
+#pragma unroll
+    for (int u = 0; u < kHand; ++u) ok &= count[u] > 0;
+    return ok;
+}
+
+// entries_of a child's row (beyond it -1), given back
+__device__ __forceinline__ void give_back(const ForkArgs& a, int32_t* row, int64_t j0, int step, const int (&page)[kHand])
+{
+    int held[kHand];
+#pragma unroll
+    for (int u = 0; u < kHand; ++u) {
+        if (page[u] != -1) row[j0 + u * step] = -1;
         held[u] = page[u] >= 0 && page[u] < a.num_pages ? atomicSub(&a.refcounts[page[u]], 1) : page[u] == -1;
     }
 #pragma unroll
-    for (int u = 0; u < kChunk / 32; ++u) {
+    for (int u = 0; u < kHand; ++u) {
         if (held[u] > 0) continue;                   // (an entry that names no page, or a free one)
         if (page[u] >= 0 && page[u] < a.num_pages) atomicAdd(&a.refcounts[page[u]], 1);
         report(a.status_word, GDN_ERR_BAD_INDEX);
     }
 }
 
-// The pages that forks take.  ALL: with the checks of the forks and the giving back before it, where there are few entries; many are given
-// back by a kernel of their own, as their atomics want more SMs than a cluster has.
-template <bool ALL>
+// The checks of the forks and the giving back, a CTA or a cluster for each fork: its atomics want more SMs than the planning cluster has.
+// (No parent is a child: the rows that are checked here are not those that change.)
+__global__ void __launch_bounds__(kThreads) give_back_kernel(const ForkArgs a)
+{
+    __shared__ int box[kCluster];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int ctas = (int)cluster.num_blocks(), i = blockIdx.x / ctas, W = a.row_pages;
+    const int me = (int)(cluster.block_rank() * blockDim.x + threadIdx.x), all = (int)(ctas * blockDim.x);
+    allow_successor();
+    cluster.sync();                                  // (all CTAs are there: they write to each other's memory)
+    wait_for_predecessor();
+    const int p = a.parents[i], c = a.children[i], n = a.tokens[i];
+    const int need = n < 0 ? -1 : n / a.page_tokens + (n % a.page_tokens > 0);
+    const bool there = p >= 0 && p < a.num_rows && c >= 0 && c < a.num_rows && need >= 0 && need <= W;
+    const int32_t* from = a.tables + (int64_t)(there ? p : 0) * W;
+    int32_t* row = a.tables + (int64_t)(there ? c : 0) * W;
+    bool bad = !there;
+    for (int k = threadIdx.x; k < a.count; k += blockDim.x) {
+        const int other = a.children[k];
+        bad |= other == p || (other == c && k != i);
+    }
+    for (int64_t j0 = me; there && j0 < need; j0 += (int64_t)all * kHand) bad |= !all_held(a, from, j0, all, need);
+    bad = __syncthreads_or(bad);
+    if (ctas > 1) {                                  // (a fork's checks are all made before any of its entries changes)
+        int wrong;
+        scan_cluster(bad, &wrong, box);
+        bad = wrong > 0;
+    }
+    if (me == 0) {
+        a.plan.need[i] = bad ? -1 : need;
+        if (bad) report(a.status_word, GDN_ERR_BAD_INDEX);
+    }
+    if (bad) return;
+    for (int64_t j0 = me; j0 < W; j0 += (int64_t)all * kHand) {
+        int page[kHand];                             // (read ahead of the checks the children of many forks keep each other waiting)
+        entries_of(row, j0, all, W, -1, page);
+        give_back(a, row, j0, all, page);
+    }
+}
+
+// The pages that forks take: the free ones, ranked by number.
 __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a)
 {
     extern __shared__ int32_t forks[];               // [count] each: parent, child, pages that the child takes (the last one in part; -1: no
-    __shared__ int part[kThreads / 32], box[kCluster];          // fork), whole pages; then the rows that are children: once or more; more than once
+    __shared__ int part[kThreads / 32], box[kCluster];          // fork), whole pages
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, lane = tid % 32, F = a.count, W = a.row_pages;
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks(), tid = threadIdx.x, F = a.count, W = a.row_pages;
     int32_t *parent = forks, *child = forks + F, *need = forks + 2 * F, *whole = forks + 3 * F;
-    uint32_t *named = reinterpret_cast<uint32_t*>(forks + 4 * F), *twice = named + (a.num_rows + 31) / 32;
-    if (ALL)
-        for (int i = tid; i < (a.num_rows + 31) / 32; i += kThreads) named[i] = twice[i] = 0;
     cluster.sync();                                  // (all CTAs are there: they write to each other's memory)
     wait_for_predecessor();
     for (int i = tid; i < F; i += kThreads) {
-        const int p = a.parents[i], c = a.children[i], n = a.tokens[i];
-        parent[i] = p;
-        child[i] = c;
+        const int n = a.tokens[i];
+        parent[i] = a.parents[i];
+        child[i] = a.children[i];
+        need[i] = a.plan.need[i];
         whole[i] = n < 0 ? 0 : n / a.page_tokens;
-        if (ALL) {
-            need[i] = n < 0 ? -1 : whole[i] + (n % a.page_tokens > 0);
-            if (c < 0 || c >= a.num_rows) continue;
-            const uint32_t bit = 1u << (c & 31);
-            if (atomicOr(&named[c >> 5], bit) & bit) atomicOr(&twice[c >> 5], bit);
-        } else {
-            need[i] = a.plan.need[i];
-        }
     }
-    __syncthreads();
-    const int chunks = (W + kChunk - 1) / kChunk, items = F * chunks, warps = ctas * (kThreads / 32), first = rank * (kThreads / 32) + tid / 32;
-    if (ALL) {
-        auto has = [](const uint32_t* set, int r) { return (set[r >> 5] >> (r & 31)) & 1u; };
-        for (int i = tid; i < F; i += kThreads) {
-            const int p = parent[i], c = child[i];
-            if (!(p >= 0 && p < a.num_rows && c >= 0 && c < a.num_rows && need[i] <= W && !has(twice, c) && !has(named, p))) need[i] = -1;
-        }
-        cluster.sync();
-        // a warp takes kChunk entries of a parent's row at a time, all of them on their way at once
-        for (int e = first; e < items; e += warps) {
-            const int i = e / chunks, j0 = (e - i * chunks) * kChunk + lane, n = need[i];
-            const int32_t* row = a.tables + (int64_t)(n > 0 ? parent[i] : 0) * W;
-            int page[kChunk / 32];
-#pragma unroll
-            for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < n ? row[j0 + 32 * u] : 0;
-            bool bad = false;
-#pragma unroll
-            for (int u = 0; u < kChunk / 32; ++u) bad |= page[u] < 0 || page[u] >= a.num_pages;
-            if (bad)                                 // (others may read either: the fork is left out by then)
-                for (int r = 0; r < ctas; ++r) *(volatile int32_t*)(cluster.map_shared_rank(need, r) + i) = -1;
-        }
-        cluster.sync();
-        for (int i = rank * kThreads + tid; i < F; i += ctas * kThreads)
-            if (need[i] < 0) report(a.status_word, GDN_ERR_BAD_INDEX);
-        for (int e = first; e < items; e += warps) {
-            const int i = e / chunks;
-            if (need[i] >= 0) give_back(a, child[i], (e - i * chunks) * kChunk + lane);
-        }
-        cluster.sync();
-    }
-    allow_successor();
-    // free pages, ranked by number: each CTA counts those of its share of the pages, then lists the first `wanted`
-    int wanted = 0;
+    int wanted = 0;                                  // (a thread reads what it wrote itself)
     for (int i = tid; i - tid < F; i += kThreads) wanted += __syncthreads_count(i < F && need[i] > whole[i]);
+    allow_successor();                               // (earlier, its CTAs take the SMs where the giving back still runs)
+    // each CTA counts the free pages of its share, then lists the first `wanted`
     const int slice = (a.num_pages + ctas - 1) / ctas, lo = min(rank * slice, a.num_pages), hi = min(lo + slice, a.num_pages);
     int mine = 0, there, all_free;
     for (int p = lo + tid; p < hi; p += kThreads) mine += __ldcg(&a.refcounts[p]) <= 0;
@@ -236,42 +256,6 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(const ForkArgs a)
             report(a.status_word, GDN_ERR_NO_PAGES);
         }
         a.plan.src[i] = src; a.plan.dst[i] = dst; a.plan.share[i] = share;
-    }
-}
-
-// The giving back of many entries, each warp for kChunk of a fork's, with the checks of the fork that fork_plan_kernel makes otherwise.
-// (No parent is a child: the rows that are checked here are not those that change.)
-__global__ void __launch_bounds__(256) give_back_kernel(const ForkArgs a)
-{
-    allow_successor();
-    wait_for_predecessor();
-    const int W = a.row_pages, chunks = (W + kChunk - 1) / kChunk, items = a.count * chunks, lane = threadIdx.x % 32;
-    for (int e = (blockIdx.x * blockDim.x + threadIdx.x) / 32; e < items; e += gridDim.x * blockDim.x / 32) {
-        const int i = e / chunks, p = a.parents[i], c = a.children[i], n = a.tokens[i];
-        const int need = n < 0 ? -1 : n / a.page_tokens + (n % a.page_tokens > 0);
-        bool ok = p >= 0 && p < a.num_rows && c >= 0 && c < a.num_rows && need >= 0 && need <= W;
-        int times = 0;
-        bool named = false;
-        for (int k = lane; k < a.count; k += 32) {
-            const int other = a.children[k];
-            times += other == c;
-            named |= other == p;
-        }
-        ok = ok && __reduce_add_sync(0xffffffffu, times) == 1 && !__any_sync(0xffffffffu, named);
-        bool bad = false;
-        for (int j0 = lane; ok && j0 < need; j0 += kChunk) {
-            int page[kChunk / 32];
-#pragma unroll
-            for (int u = 0; u < kChunk / 32; ++u) page[u] = j0 + 32 * u < need ? a.tables[(int64_t)p * W + j0 + 32 * u] : 0;
-#pragma unroll
-            for (int u = 0; u < kChunk / 32; ++u) bad |= page[u] < 0 || page[u] >= a.num_pages;
-        }
-        ok = ok && !__any_sync(0xffffffffu, bad);
-        if (e == i * chunks && lane == 0) {
-            a.plan.need[i] = ok ? need : -1;
-            if (!ok) report(a.status_word, GDN_ERR_BAD_INDEX);
-        }
-        if (ok) give_back(a, c, (e - i * chunks) * kChunk + lane);
     }
 }
 
@@ -415,12 +399,10 @@ unsigned grid_for(uint64_t pieces, uint64_t entries)
 }
 
 // CTAs of a planning kernel: one where little is to be read, whose barriers cost least, else a cluster
-unsigned plan_ctas(int64_t pages, int64_t entries) { return pages <= 8192 && entries <= 8192 ? 1 : kCluster; }
-constexpr int64_t kFewEntries = 16384;
-
+unsigned plan_ctas(int64_t pages) { return pages <= 8192 ? 1 : kCluster; }
 }  // namespace
 
-int fork_launches(const gdn_cache_desc* d, int32_t count) { return ((int64_t)count * d->row_pages <= kFewEntries ? 1 : 2) + pool_launches(d); }
+int fork_launches(const gdn_cache_desc* d) { return 2 + pool_launches(d); }
 
 int pool_launches(const gdn_cache_desc* d) { return d->num_pools > 0 ? (d->num_pools + kPoolsPerLaunch - 1) / kPoolsPerLaunch : 1; }
 
@@ -442,17 +424,17 @@ cudaError_t launch_cache_fork(const gdn_cache_desc* d, int32_t* refcounts, int32
     int32_t* w = (int32_t*)d->workspace;
     a.plan = {w, w + count, w + 2 * (int64_t)count, w + 3 * (int64_t)count, w + 4 * (int64_t)count};
     const int64_t entries = (int64_t)count * d->row_pages;
-    const bool all = entries <= kFewEntries;
-    const size_t smem = 4 * sizeof(int32_t) * (size_t)count + (all ? 2 * sizeof(uint32_t) * ((d->num_rows + 31) / 32) : 0);
+    const size_t smem = 4 * sizeof(int32_t) * (size_t)count;
     cudaStream_t stream = (cudaStream_t)d->stream;
+    // A fork's CTAs and their threads: one small one for short rows, of which an SM runs more at once, a cluster for long rows.  (us of a call,
+    // 128 / 512 threads: 4,096 forks with rows of 64 entries 46 / 62, 512 of 64 13.1 / 15.1, 32 of 256 10.6 / 10.4, 64 of 1,024 15.1 / 13.4.
+    // One CTA / a cluster: 64 forks with rows of 4,096 20.4 / 23.5, of 8,192 38 / 31; 16 of 16,384 38 / 20.)
+    const unsigned per_fork = d->row_pages <= 4096 ? 1 : kCluster, threads = d->row_pages <= 256 ? 128 : kThreads, ctas = plan_ctas(d->num_pages);
     cudaError_t e = cudaSuccess;
-    auto plan = all ? fork_plan_kernel<true> : fork_plan_kernel<false>;
     // (the most that any call needs: another thread's call may set it too)
-    constexpr int most = 4 * sizeof(int32_t) * GDN_CACHE_MAX_FORKS + 2 * sizeof(uint32_t) * (GDN_CACHE_MAX_ROWS / 32);
-    if (smem > 40 * 1024) e = cudaFuncSetAttribute(plan, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    const unsigned ctas = plan_ctas(d->num_pages, all ? entries : 0);
-    if (e == cudaSuccess && !all) e = launch_kernel(give_back_kernel, grid_for(0, entries), 256, 0, stream, 1, a);
-    if (e == cudaSuccess) e = launch_kernel(plan, ctas, kThreads, smem, stream, ctas, a);
+    if (smem > 40 * 1024) e = cudaFuncSetAttribute(fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * sizeof(int32_t) * GDN_CACHE_MAX_FORKS);
+    if (e == cudaSuccess) e = launch_kernel(give_back_kernel, count * per_fork, threads, 0, stream, per_fork, a);
+    if (e == cudaSuccess) e = launch_kernel(fork_plan_kernel, ctas, kThreads, smem, stream, ctas, a);
     for (int i = 0; i < pool_launches(d) && e == cudaSuccess; ++i) {
         const Pools p = pools_from(d, i * kPoolsPerLaunch);
         const unsigned sharing = i == 0 ? grid_for(0, entries) : 0;
@@ -474,7 +456,7 @@ cudaError_t launch_cache_compact(const gdn_cache_desc* d, const int32_t* refcoun
     int32_t* w = (int32_t*)d->workspace;
     a.plan = {w, w + 64, w + 64 + (int64_t)d->num_pages, w + 64 + 2 * (int64_t)d->num_pages};
     cudaStream_t stream = (cudaStream_t)d->stream;
-    const unsigned ctas = plan_ctas(d->num_pages, 0);
+    const unsigned ctas = plan_ctas(d->num_pages);
     cudaError_t e = launch_kernel(compact_plan_kernel, ctas, kThreads, 0, stream, ctas, a);
     for (int i = 0; i < pool_launches(d) && e == cudaSuccess; ++i) {
         const Pools p = pools_from(d, i * kPoolsPerLaunch);
