@@ -398,8 +398,10 @@ unsigned grid_for(uint64_t pieces, uint64_t entries)
     return (unsigned)(ctas < 1 ? 1 : ctas > 148 * 4 ? 148 * 4 : ctas);
 }
 
-// CTAs of a planning kernel: one where little is to be read, whose barriers cost least, else a cluster
-unsigned plan_ctas(int64_t pages) { return pages <= 8192 ? 1 : kCluster; }
+// CTAs of a planning kernel: one where few counts are to be read, whose barriers cost least, else a cluster.  (us with one / a cluster: a
+// compaction of 600 pages 5.4 / 6.0, 1,024 5.7 / 5.9, 1,500 6.6 / 6.2, 8,192 17.1 / 7.3; a fork among 929 pages 8.0 / 8.4, 64 among 4,224
+// 12.6 / 12.3, among 65,664 53 / 31.)
+unsigned plan_ctas(int64_t pages) { return pages <= 1024 ? 1 : kCluster; }
 }  // namespace
 
 int fork_launches(const gdn_cache_desc* d) { return 2 + pool_launches(d); }
