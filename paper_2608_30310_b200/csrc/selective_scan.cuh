@@ -178,8 +178,8 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
             bp += TB * a.b_stride; cp += TB * a.c_stride;
         };
         auto commit = []() { asm volatile("cp.async.commit_group;" ::: "memory"); };
-        // (dt, dt x) and (b, c) of a block.  Rows past the request's end become zeros, whatever lies there: the state and the sums of the
-        // rows before do not see them.
+        // (dt, dt x) and (b, c) of a block.  Rows past the request's end become zeros, whatever lies there.  (The state does not take them in
+        // either: with a = -inf a time step of zero is no number.)
         auto prepare = [&](int block) {
             const int slot = block % kRing, buf = block & 1, left = req.y - req.x - block * TB;
             Pack<T, V8> b[BPT], c[BPT];
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
         const float* ps = &sh.p[buf][F::p_at(ch0)];
         const uint32_t *b0 = &sh.bc[buf][0][ln * SS], *b1 = &sh.bc[buf][F::BC - 1][ln * SS];
         float* ys = &sh.y[buf][F::y_at(ch0)];                // (CC channels are neighbours there)
-        auto rows_of = [&](int t, float* sums) {
+        auto rows_of = [&](int t, float* sums, bool real) {                   // (not real: past the request's end, the state stays)
             float b[SS], c[SS], p[2 * CC];
             const Pack<uint32_t, SS> w = *reinterpret_cast<const Pack<uint32_t, SS>*>(b0 + t * S);
             if constexpr (sizeof(T) == 2) {
@@ -308,8 +308,9 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
             for (int k = 0; k < CC; ++k) {
                 const float dt = p[2 * k], dx = p[2 * k + 1];
                 if constexpr (SS == 1) {
-                    h[k][0] = fmaf(ex2(fmaf(dt, a2[k][0], kLift)), h[k][0], dx * b[0]);
-                    sums[k] = h[k][0] * c[0];
+                    const float hn = fmaf(ex2(fmaf(dt, a2[k][0], kLift)), h[k][0], dx * b[0]);
+                    h[k][0] = real ? hn : h[k][0];
+                    sums[k] = hn * c[0];
                 } else {
                     F2 acc;
 #pragma unroll
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
                         const float2 e = parts(fma(pair(dt, dt), pair(a2[k][s], a2[k][s + 1]), both(kLift)));
                         const F2 hn = fma(pair(ex2(e.x), ex2(e.y)), pair(h[k][s], h[k][s + 1]), mul(pair(dx, dx), pair(b[s], b[s + 1])));
                         const float2 hv = parts(hn);
-                        h[k][s] = hv.x; h[k][s + 1] = hv.y;
+                        h[k][s] = real ? hv.x : h[k][s]; h[k][s + 1] = real ? hv.y : h[k][s + 1];
                         acc = s ? fma(hn, pair(c[s], c[s + 1]), acc) : mul(hn, pair(c[s], c[s + 1]));
                     }
                     const float2 r = parts(acc);
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
             for (int t = 0; t < left; t += TS) {
                 float sums[F::SUMS];
 #pragma unroll
-                for (int i = 0; i < TS; ++i) rows_of(t + i, &sums[i * CC]);
+                for (int i = 0; i < TS; ++i) rows_of(t + i, &sums[i * CC], t + i < left);
                 reduce(sums);
                 store(t, sums);
             }
@@ -365,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
                 float sums[F::SUMS];
                 if (t < TB)
 #pragma unroll
-                    for (int i = 0; i < TS; ++i) rows_of(t + i, &sums[i * CC]);
+                    for (int i = 0; i < TS; ++i) rows_of(t + i, &sums[i * CC], true);
                 if (t > 0) {
                     reduce(before);
                     store(t - TS, before);
