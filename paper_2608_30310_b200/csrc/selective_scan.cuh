@@ -14,6 +14,7 @@
 // slots, unit and shared memory are 68-73 % busy.  One request of 1,638 tokens: 62 us (unit 28), one compute and one helper warp per
 // scheduler, latency.  Everything in every warp, without roles, took 1,050 and 174 us.  32 rows a block: sixteen 334 us for eight hits.
 #pragma once
+#include <float.h>
 #include "layers.cuh"
 
 namespace gdn {
@@ -284,7 +285,11 @@ __global__ void __launch_bounds__(kThreads, F::SS * F::CC > 4 ? 2 : 3) selective
             if (from >= 0) load_values<float, SS>(a.init_state + ((int64_t)from * a.channels + ch) * S + ln * SS, h[c]);
         }
 #pragma unroll
-        for (int s = 0; s < SS; ++s) a2[c][s] *= kLog2e;
+        for (int s = 0; s < SS; ++s) {
+            const float a = a2[c][s];                        // (one that is finite stays so: a time step of 0 leaves the state as it is)
+            a2[c][s] *= kLog2e;
+            if (isinf(a2[c][s]) && !isinf(a)) a2[c][s] = copysignf(FLT_MAX, a);
+        }
     }
     __syncthreads();
     for (int block = 0; block < blocks; ++block) {

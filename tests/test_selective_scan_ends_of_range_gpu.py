@@ -1,4 +1,4 @@
-"""The selective scan with decays at the ends of the range: a of minus infinity (a state that holds one token)."""
+"""The selective scan with decays at the ends of the range: a of minus infinity (a state that holds one token), and of the type's lowest value."""
 import pytest
 import torch
 
@@ -48,3 +48,18 @@ def test_a_of_minus_infinity(dtype, S, C, lens):
     a = m["a"].clone()
     a[a == -1e30] = -float("inf")
     check(m, a, lens, True, init)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("S", [8, 16, 32, 64])
+@pytest.mark.parametrize("C,lens", CALLS, ids=str)
+def test_a_at_the_lowest_value(dtype, S, C, lens):
+    """Time steps of 0 leave the state as it is whatever a is; others leave nothing of it."""
+    m = scan_inputs(sum(lens), C, S, 1, dtype, S + 1)
+    init = torch.randn((len(lens), C, S), generator=torch.Generator().manual_seed(3))
+    low = torch.finfo(torch.float32).min
+    m["a"][:, S // 3] = low
+    m["a"][C // 2] = low
+    m["dt"] = m["dt"].abs() + 0.01
+    m["dt"][::2] = 0
+    check(m, m["a"], lens, False, init)
