@@ -216,7 +216,7 @@ GDN_API int64_t tail_select(int64_t prefix_len, double budget_frac);
  * ---- Recurrent layers beside the Gated DeltaNet: short convolution and selective scan ----
  *
  * What stands before and beside the recurrence above in hybrid models.  Device pointers only, of the current device.  Prompts are packed as above
- * (cu_tail_lens: request n owns rows [cu[n], cu[n+1])); total_tokens may exceed cu[num_seqs] (a padded batch): rows from
+ * (cu_tail_lens: request n owns rows [cu[n], cu[n+1]); 2^31 - 64 rows at most); total_tokens may exceed cu[num_seqs] (a padded batch): rows from
  * cu[num_seqs] on, and those before cu[0] where the list is a slice of a longer batch's, are neither read nor written.  Row strides are in elements, between consecutive tokens; the last dimension is
  * packed.  Rows may begin anywhere that their values may (aligned ones are faster: 8 bytes for the convolution, up to 16 for the scan); the
  * pools, and a of the scan, are 16-byte aligned.  The states lie in pools:
@@ -338,7 +338,8 @@ GDN_API int32_t gdn_cache_copy(const gdn_cache_desc* desc, const int32_t* src, c
  * count above 0.  A fork that breaks this is left out, its child's row as it was (GDN_ERR_BAD_INDEX).  (A page's count is at least the number
  * of entries that name it, as the calls leave it; whether a smaller one that is not 0 serves is not defined.)  A child's entries are given
  * back as by gdn_cache_free.  Too few free pages: the forks that get none, the last ones
- * that need one, leave their child's row empty (GDN_ERR_NO_PAGES).  At most GDN_CACHE_MAX_ROWS rows and GDN_CACHE_MAX_FORKS forks.
+ * that need one, leave their child's row empty (GDN_ERR_NO_PAGES).  At most GDN_CACHE_MAX_ROWS rows, GDN_CACHE_MAX_FORKS forks
+ * and 2^30 pages.
  */
 #define GDN_CACHE_MAX_ROWS 262144
 #define GDN_CACHE_MAX_FORKS 4096
@@ -355,7 +356,8 @@ GDN_API int32_t gdn_cache_free(const gdn_cache_desc* desc, int32_t* refcounts, i
  * The live pages (count above 0) brought to the front: with M of them, the k-th live page at or after M moves into the k-th free
  * page below M.  out_refcounts and out_tables receive the counts and tables afterwards (they may be the inputs; where they are not,
  * the old tables stay valid to read by until the pages moved from are written again), page_map [num_pages] each page's new number
- * (-1: free), live [1] M.  A table entry that names no live page becomes -1 (GDN_ERR_BAD_INDEX).
+ * (-1: free), live [1] M.  A table entry that names no live page becomes -1 (GDN_ERR_BAD_INDEX).  At most
+ * 2^30 pages.
  */
 GDN_API int32_t gdn_cache_compact(const gdn_cache_desc* desc, const int32_t* refcounts, const int32_t* tables, int32_t* out_refcounts,
                                   int32_t* out_tables, int32_t* page_map, int32_t* live);

@@ -15,12 +15,16 @@ int32_t done(cudaError_t e, int launches)
     return GDN_OK;
 }
 
+// Rows of a packed batch, and pages that a call ranks: the kernels add up to a block's rows, or a CTA's threads and a share's rounding, to their numbers in 32 bits.
+constexpr int64_t kMostRows = 0x7fffffffLL - 63;
+constexpr int32_t kMostPages = 1 << 30;
+
 // What the two layers have in common.  `step`: one token per request, states in and out.
 int32_t check_layer(int32_t channels, int32_t io_dtype, int32_t num_seqs, int64_t total, int32_t num_init, int32_t num_out, const int32_t* cu,
                     const int32_t* init_slots, const int32_t* out_slots, const int32_t* status_word, const void* state_in, const void* state_out, bool step)
 {
     if (channels <= 0 || num_seqs < 0 || (io_dtype != GDN_F32 && io_dtype != GDN_BF16)) return GDN_ERR_INVALID_ARG;
-    if (!step && (total < 0 || total > 0x7fffffffLL || !cu || !aligned(cu, 4))) return GDN_ERR_INVALID_ARG;
+    if (!step && (total < 0 || total > kMostRows || !cu || !aligned(cu, 4))) return GDN_ERR_INVALID_ARG;
     if (step && (!state_in || !state_out)) return GDN_ERR_INVALID_ARG;
     if (!aligned(init_slots, 4) || !aligned(out_slots, 4) || !aligned(status_word, 4) || !aligned(state_in, 16) || !aligned(state_out, 16))
         return GDN_ERR_INVALID_ARG;
@@ -171,7 +175,7 @@ int32_t gdn_cache_fork(const gdn_cache_desc* d, int32_t* refcounts, int32_t* tab
     int32_t rc = check_cache(d, true, count, true);
     if (rc != GDN_OK) return rc;
     if (d->page_tokens <= 0) return GDN_ERR_INVALID_ARG;
-    if (d->num_rows > GDN_CACHE_MAX_ROWS || count > GDN_CACHE_MAX_FORKS) return GDN_ERR_UNSUPPORTED;
+    if (d->num_pages > kMostPages || d->num_rows > GDN_CACHE_MAX_ROWS || count > GDN_CACHE_MAX_FORKS) return GDN_ERR_UNSUPPORTED;
     if (count == 0) return GDN_OK;
     if (!ints(refcounts) || !ints(tables) || !ints(parents) || !ints(children) || !ints(tokens)) return GDN_ERR_INVALID_ARG;
     if ((rc = check_workspace(d, count)) != GDN_OK) return rc;
@@ -192,6 +196,7 @@ int32_t gdn_cache_compact(const gdn_cache_desc* d, const int32_t* refcounts, con
 {
     int32_t rc = check_cache(d, true, 0, true);
     if (rc != GDN_OK) return rc;
+    if (d->num_pages > kMostPages) return GDN_ERR_UNSUPPORTED;
     if (!ints(refcounts) || !ints(tables) || !ints(out_refcounts) || !ints(out_tables) || !ints(page_map) || !ints(live)) return GDN_ERR_INVALID_ARG;
     if ((rc = check_workspace(d, 0)) != GDN_OK) return rc;
     return done(gdn::launch_cache_compact(d, refcounts, tables, out_refcounts, out_tables, page_map, live), 1 + gdn::pool_launches(d));
