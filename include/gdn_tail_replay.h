@@ -255,7 +255,7 @@ GDN_API int32_t gdn_short_conv(const gdn_conv_desc* desc, const void* x, const v
 /*
  * The same for one token per request: x and out [N, C].  Request n has slot init_slots[n] (NULL: n) of both pools; one with a
  * negative slot is padding, whose row of out and states are left as they were.  out_slots and total_tokens are ignored.  out may be
- * x, state_out may be state_in.
+ * x (the same address and stride), state_out may be state_in.
  */
 GDN_API int32_t gdn_short_conv_step(const gdn_conv_desc* desc, const void* x, const void* weight, const void* bias,
                                     const void* state_in, void* out, void* state_out);

@@ -45,6 +45,12 @@ struct Rows {
     }
 };
 
+// Whether `out` begins where an input does but its rows lie elsewhere: one row's result would replace another row's input.
+inline bool crosses(const void* out, int64_t out_stride, const void* in, int64_t stride, int64_t rows)
+{
+    return rows > 1 && out && out == in && out_stride != stride;
+}
+
 int32_t conv(const gdn_conv_desc* d, const void* x, const void* weight, const void* bias, const int32_t* cu, const void* state_in, void* out,
              void* state_out, bool step)
 {
@@ -58,6 +64,7 @@ int32_t conv(const gdn_conv_desc* d, const void* x, const void* weight, const vo
     const Rows rows_ok{step ? d->num_seqs : d->total_tokens, e};
     if (!rows_ok(x, d->x_stride, d->channels) || !rows_ok(out, d->out_stride, d->channels)) return GDN_ERR_INVALID_ARG;
     if (!step && out == x && x) return GDN_ERR_INVALID_ARG;
+    if (crosses(out, d->out_stride, x, d->x_stride, rows_ok.rows)) return GDN_ERR_INVALID_ARG;
     if (d->width < 2 || d->width > 4) return GDN_ERR_UNSUPPORTED;
     if (d->num_seqs == 0) return GDN_OK;
     gdn::ConvArgs a = {};
@@ -83,6 +90,9 @@ int32_t scan(const gdn_scan_desc* d, const void* x, const void* dt, const float*
     const Rows rows_ok{step ? d->num_seqs : d->total_tokens, e};
     if (!rows_ok(x, d->x_stride, d->channels) || !rows_ok(dt, d->dt_stride, d->channels) || !rows_ok(out, d->out_stride, d->channels) ||
         !rows_ok(b, d->b_stride, bc) || !rows_ok(c, d->c_stride, bc) || (z && !rows_ok(z, d->z_stride, d->channels)))
+        return GDN_ERR_INVALID_ARG;
+    if (crosses(out, d->out_stride, x, d->x_stride, rows_ok.rows) || crosses(out, d->out_stride, dt, d->dt_stride, rows_ok.rows) ||
+        crosses(out, d->out_stride, z, d->z_stride, rows_ok.rows))
         return GDN_ERR_INVALID_ARG;
     if (d->states != 8 && d->states != 16 && d->states != 32 && d->states != 64) return GDN_ERR_UNSUPPORTED;
     if (d->num_seqs == 0) return GDN_OK;
