@@ -137,17 +137,19 @@ class Workspace:
 
     The CTAs of a call hand each other operands through the buffer, so that calls which may overlap on the GPU need one each: every
     stream has its own, allocated for that stream.  ``buf`` is that of the stream that came first.  A captured call keeps the
-    address of its capture stream's buffer; buffers that device calls can have used are therefore kept when they are outgrown, as
-    long as the object lives.  Keep it as long as the graph, and let no replay overlap another, or a call on the capture stream."""
+    address of its capture stream's buffer; buffers that device calls have used are therefore kept when they are outgrown, as
+    long as the object lives (those of other calls, which stage host memory, are given back).  Keep it as long as the graph, and let no replay overlap another, or a call on the capture stream."""
 
-    # More than any call on device memory needs (37 chains x 9 slots x 33,280 bytes and the request list); such a call takes a
-    # buffer of this size or, without the operand ring, a small one, so that few are ever outgrown.
+    # More than a replay on device memory needs (37 chains x 9 slots x 33,280 bytes and the request list); such a call takes a
+    # buffer of this size or, without the operand ring, a small one, so that few are ever outgrown.  Every buffer up to this size is
+    # kept; of the larger ones, those in `kept`.
     SMALL, DEVICE = 64 << 10, 12 << 20
 
     def __init__(self, device="cuda"):
         self.device = device
         self.by_stream = {}                  # stream handle -> buffer; read by the native argument path
         self.outgrown = []
+        self.kept = {}                       # stream handle -> its buffer, where a device call has used one larger than DEVICE; likewise
 
     @property
     def buf(self):
@@ -158,22 +160,26 @@ class Workspace:
         """Takes ``t`` as the buffer of the current stream in place of all others (None: gives them back)."""
         self.by_stream.clear()
         self.outgrown.clear()
+        self.kept.clear()
         if t is not None:
             import torch
             self.by_stream[int(torch.cuda.current_stream().cuda_stream)] = t
 
-    def reserve(self, nbytes: int, stream, current: bool = False):
-        """The buffer of ``stream`` (``current``: known to be the current one), of at least ``nbytes`` bytes."""
+    def reserve(self, nbytes: int, stream, current: bool = False, device_call: bool = False):
+        """The buffer of ``stream`` (``current``: known to be the current one), of at least ``nbytes`` bytes; a ``device_call``, which may be
+        captured, keeps it."""
         import torch
         handle = int(stream.cuda_stream)
         buf = self.by_stream.get(handle)
         if buf is None or buf.numel() < nbytes:
-            if buf is not None and buf.numel() <= self.DEVICE + 256:
+            if buf is not None and (buf.numel() <= self.DEVICE + 256 or self.kept.pop(handle, None) is buf):
                 self.outgrown.append(buf)
             size = max(int(nbytes), 256 if nbytes <= self.SMALL else self.DEVICE) + 256
             with contextlib.nullcontext() if current else _on_stream(stream):
                 buf = torch.empty(size, dtype=torch.uint8, device=self.device)
             self.by_stream[handle] = buf
+        if device_call and buf.numel() > self.DEVICE + 256:
+            self.kept[handle] = buf
         return buf
 
     def ensure(self, nbytes: int, stream=None):
@@ -250,7 +256,7 @@ def _forward(fn_name, q, k, v, g, beta, cu_tail_lens, chunk, out_o, out_state, *
         if workspace is None:
             workspace = Workspace(device="cuda" if host else q.device)
         if type(workspace) is Workspace:
-            buf = workspace.reserve(need, stream, current)
+            buf = workspace.reserve(need, stream, current, device_call=not host)
             desc.workspace, desc.workspace_bytes = _aligned(buf)
         else:
             desc.workspace, desc.workspace_bytes = workspace.ensure(need)

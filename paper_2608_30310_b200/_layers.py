@@ -265,12 +265,9 @@ def _scratch(lib, desc, count, workspace, stream):
     current = stream is None
     if current:
         stream = torch.cuda.current_stream()
-    old = workspace.by_stream.get(int(stream.cuda_stream))
-    buf = workspace.reserve(need, stream, current)
+    buf = workspace.reserve(need, stream, current, device_call=True)
     if not buf.is_cuda or buf.device.index != torch.cuda.current_device():
         raise ValueError("workspace must be on the current device")
-    if old is not None and old is not buf and not any(x is old for x in workspace.outgrown):
-        workspace.outgrown.append(old)                    # (a captured call may have its address)
     desc.workspace, desc.workspace_bytes = B._aligned(buf)
     return buf
 

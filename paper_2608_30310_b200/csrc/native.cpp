@@ -20,7 +20,8 @@ using Decode = int32_t (*)(const gdn_desc*, const void*, const void*, const void
 Forward g_forward[3] = {};               // gdn_tail_replay, gdn_full_prefill, gdn_tail_replay_static_scratch
 Decode g_decode = nullptr;
 size_t (*g_workspace_size)(const gdn_desc*) = nullptr;
-PyObject *s_by_stream = nullptr, *s_cuda_stream = nullptr, *g_workspace_type = nullptr;
+PyObject *s_by_stream = nullptr, *s_cuda_stream = nullptr, *s_kept = nullptr, *g_workspace_type = nullptr;
+int64_t g_device_bytes = 0;              // Workspace.DEVICE
 
 inline const at::Tensor* tensor(PyObject* o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
 // contiguous, of type dt, on the side given by `cuda`, of shape {s...}
@@ -81,6 +82,15 @@ struct Ref {                                 // an owned reference, given back o
     ~Ref() { Py_XDECREF(o); }
 };
 
+// Whether a device call, which may be captured, may take the Workspace's buffer: a larger one than such calls need is perhaps the staging of
+// calls on host memory, which goes when it is outgrown, until the general path has put it down as kept.
+bool kept_when_outgrown(PyObject* workspace, PyObject* key, PyObject* buffer, int64_t bytes)
+{
+    if (bytes <= g_device_bytes + 256) return true;
+    const Ref map{PyObject_GetAttr(workspace, s_kept)};
+    return map.o && PyDict_Check(map.o) && PyDict_GetItemWithError(map.o, key) == buffer;
+}
+
 // forward(which, q, k, v, g, beta, cu_tail_lens, chunk, out_o, out_state, init_state, workspace, status_word, kernel, stream, raw)
 PyObject* forward(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -125,7 +135,7 @@ PyObject* forward(PyObject*, PyObject* const* a, Py_ssize_t n)
         Py_XINCREF(b.o);                                  // (held over the call: another thread may let the Workspace grow)
         const at::Tensor* buf = b.o ? tensor(b.o) : nullptr;
         const int64_t need = (int64_t)g_workspace_size(&d);
-        const bool ok = buf && buf->is_cuda() && buf->element_size() == 1 && buf->numel() >= need;
+        const bool ok = buf && buf->is_cuda() && buf->element_size() == 1 && buf->numel() >= need && (!cuda || kept_when_outgrown(a[11], key.o, b.o, buf->numel()));
         if (ok) {
             const uintptr_t base = (uintptr_t)buf->data_ptr(), off = (256 - base % 256) % 256;
             d.workspace = (void*)(base + off);
@@ -177,6 +187,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
     for (int i = 0; i < 3; ++i) g_forward[i] = (Forward)p[i];
     g_decode = (Decode)p[3];
     g_workspace_size = (size_t (*)(const gdn_desc*))p[4];
+    const Ref bytes{PyObject_GetAttrString(a[5], "DEVICE")};
+    g_device_bytes = bytes.o ? PyLong_AsLongLong(bytes.o) : 0;
+    if (PyErr_Occurred()) return nullptr;
     Py_INCREF(a[5]);
     Py_XSETREF(g_workspace_type, a[5]);
     Py_RETURN_NONE;
@@ -257,7 +270,9 @@ struct Args {
         const at::Tensor* buf = b.o ? tensor(b.o) : nullptr;
         if (!buf || !buf->is_cuda() || buf->device().index() != device || buf->element_size() != 1) return false;
         const uintptr_t at = (uintptr_t)buf->data_ptr(), off = (256 - at % 256) % 256;
-        if ((size_t)buf->numel() < need + off) return false;
+        const bool kept = kept_when_outgrown(o, key.o, b.o, buf->numel());
+        PyErr_Clear();
+        if (!kept || (size_t)buf->numel() < need + off) return false;
         base = (void*)(at + off);
         bytes = (size_t)buf->numel() - off;
         return true;
@@ -478,6 +493,7 @@ PyMODINIT_FUNC PyInit__native()
 {
     s_by_stream = PyUnicode_InternFromString("by_stream");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_kept = PyUnicode_InternFromString("kept");
     PyObject* m = PyModule_Create(&module);
     if (m && PyModule_AddStringConstant(m, "built_for_torch", BUILT_FOR_TORCH) < 0) { Py_DECREF(m); return nullptr; }
     return m;
