@@ -262,6 +262,9 @@ def _scratch(lib, desc, count, workspace, stream):
     need = int(lib.gdn_cache_workspace_size(ctypes.byref(desc), count))
     if workspace is None:
         workspace = B.Workspace(device="cuda")
+    if type(workspace) is not B.Workspace:                # (a caller's own, as the replay takes it)
+        desc.workspace, desc.workspace_bytes = workspace.ensure(need)
+        return workspace
     current = stream is None
     if current:
         stream = torch.cuda.current_stream()
