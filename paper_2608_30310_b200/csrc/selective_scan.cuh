@@ -10,8 +10,8 @@
 // barrier per block.
 //
 // Bound by its exponentials, not by memory: one result of the special-function unit per state and token, three more per channel and token.
-// Eight hits (12,616 tokens, 4,096 channels, 16 states, bf16) take 302 us where the unit alone would take 215 and the memory 65; issue
-// slots, unit and shared memory are 68-73 % busy.  One request of 1,638 tokens: 62 us (unit 28), one compute and one helper warp per
+// Eight hits (12,616 tokens, 4,096 channels, 16 states, bf16) take 301 us where the unit alone would take 215 and the memory 65; issue
+// slots, unit and shared memory are 68-73 % busy.  One request of 1,638 tokens: 61 us (unit 28), one compute and one helper warp per
 // scheduler, latency.  Everything in every warp, without roles, took 1,050 and 174 us.  32 rows a block: sixteen 334 us for eight hits.
 #pragma once
 #include <float.h>
@@ -427,11 +427,15 @@ template <typename T, typename F> cudaError_t launch_form(const ScanArgs& a, cud
 // words of b and c per state, which two channels a lane share: four states of two channels, from more states on (4,096 channels 71 with
 // two states a lane, 72 so; eight hits 445, 366; four states of one channel 398, two of two 375).  64 states are summed over 16 lanes, which two
 // channels a lane halve (bf16, 4,096 channels 205 -> 168).  With 8 states that form's tiles do not fit the shared memory in fp32: two by two.
+// The same borders at other numbers of states (700 tokens, bf16, us with one / two / the widest form): 8 states 110 per SM 16 / 22 / 36, 220 24 / 23 /
+// 37, 320 33 / 32 / 37, 700 60 / 44 / 54, 1,400 107 / 86 / 87; 32 states 110 15 / 21 / 26, 220 23 / 21 / 26, 450 42 / 30 / 27, 700 59 / 41 / 42, 1,400 104 /
+// 78 / 59; 64 states (two, the widest) 220 20 / 46, 450 30 / 47, 700 43 / 47, 1,400 82 / 74.  fp32: 8 states 700 66 / 62 / 80, 1,400 117 / 113 / 120; 32 states
+// 450 52 / 34 / 44, 700 75 / 55 / 44, 1,400 139 / 100 / 88; 64 states 450 44 / 48, 700 64 / 47, 1,400 127 / 94.
 template <typename T, int S> cudaError_t launch_states(const ScanArgs& a, cudaStream_t stream)
 {
     const int64_t per_sm = (int64_t)a.num_seqs * a.channels * S / 148;
     if (S < 64 && per_sm <= 160) return launch_form<T, Form<S, S < 64 ? 1 : 2, 1, T>>(a, stream);
-    if (per_sm <= (sizeof(T) == 2 ? 320 : 700)) return launch_form<T, Form<S, 2, 1, T>>(a, stream);
+    if (per_sm <= (sizeof(T) == 2 && S < 64 ? 320 : 700)) return launch_form<T, Form<S, 2, 1, T>>(a, stream);
     constexpr bool half = sizeof(T) == 2;
     return launch_form<T, Form<S, !half && S == 8 ? 2 : 4, half && S < 64 ? 1 : 2, T>>(a, stream);
 }
