@@ -1,8 +1,8 @@
 // One token of the selective scan per request, from and to a state in memory.
 //
 // Bound by HBM: every state is read and written once (8 bytes), for one exponential and five flops; beside that, what a channel costs (time
-// step, gate, addresses), so that a lane has eight states of a channel.  256 requests of 4,096 channels and 16 states: 27 us, 5.3 TB/s; 1,024
-// requests: 99 us, 5.8 TB/s.
+// step, gate, addresses), so that a lane has eight states of a channel.  256 requests of 4,096 channels and 16 states: 28 us, 5.1 TB/s (26 us
+// in a graph); 1,024 requests: 98 us, 5.8 TB/s.
 #include "selective_scan.cuh"
 
 namespace gdn {

@@ -6,7 +6,8 @@
 // row is read once, but for the K - 1 rows before a thread's first.  Where a request begins inside the walk, the window is refilled
 // from the request's start state, and the same thread writes the request's final state; it also goes on for the K - 1 rows that need the
 // start state, past the end of its share if need be.  So no other thread reads the start state, and both may be the same memory.  Bound by HBM, closely followed by the special-function unit (two
-// results a value, 61 % busy) and the loads' latency.  Four hits (10,094 rows of 8,192 bf16 channels): 63 us, 5.3 TB/s; 51 us at the copy rate.
+// results a value, 61 % busy) and the loads' latency.  Four hits (10,094 rows of 8,192 bf16 channels): 67 us, 4.9 TB/s (62 us in a graph); 51 us at
+// the copy rate.  One channel a thread, where the alignment or the number of channels asks for it: 182 us.
 #include "layers.cuh"
 
 namespace gdn {
@@ -215,8 +216,8 @@ cudaError_t launch(const ConvArgs& a, bool step, cudaStream_t stream)
         if (threads > 0xffffffffull - 128) return cudaErrorNotSupported;
         return launch_kernel(short_conv_step_kernel<T, K, VEC>, (unsigned)((threads + 127) / 128), 128, 0, stream, 1, a, vectors);
     }
-    // Rows per thread: two rounds of resident CTAs, but at least eight rows (four hits of 8,192 channels, 51 us at the copy rate: one round 69 us,
-    // two 66, four 68; 32 hits 357, 338, 334; 410 rows 5.9).
+    // Rows per thread: two rounds of resident CTAs, but at least eight rows (us with one / two / four rounds: four hits of 8,192 channels 62.8 / 62.0 /
+    // 62.0, the same in three calls of fewer channels 75 / 77 / 81, 32 hits 472 / 440 / 430; 410 rows 7.3 / 7.4 / 7.1).
     const int64_t threads_wanted = 2 * 148ll * kResident * 128;
     int rows = (int)((a.total_tokens * (int64_t)vectors + threads_wanted - 1) / threads_wanted);
     rows = rows < 8 ? 8 : (rows + kRows - 1) / kRows * kRows;
