@@ -218,7 +218,7 @@ GDN_API int64_t tail_select(int64_t prefix_len, double budget_frac);
  * What stands before and beside the recurrence above in hybrid models.  Device pointers only, of the current device.  Prompts are packed as above
  * (cu_tail_lens: request n owns rows [cu[n], cu[n+1]); 2^31 - 64 rows at most); total_tokens may exceed cu[num_seqs] (a padded batch): rows from
  * cu[num_seqs] on, and those before cu[0] where the list is a slice of a longer batch's, are neither read nor written.  Row strides are in elements, between consecutive tokens; the last dimension is
- * packed.  Rows may begin anywhere that their values may (aligned ones are faster: 8 bytes for the convolution, up to 16 for the scan); the
+ * packed.  Rows, weights and biases may begin anywhere that their values may (aligned ones are faster: 8 bytes for the convolution, up to 16 for the scan); the
  * pools, and a of the scan, are 16-byte aligned.  The states lie in pools:
  *     convolution  [slots, width - 1, channels] in io_dtype: the last width - 1 input rows, oldest first
  *     scan         [slots, channels, states] fp32
